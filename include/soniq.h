@@ -498,6 +498,179 @@ soniq_status soniq_plan_input_channels(const uint8_t* a_bits, int64_t K, int64_t
 soniq_status soniq_weights_unpack_debug(soniq_weights w, int32_t* codes, float* s_w);
 soniq_status soniq_act_unpack_debug(soniq_act act, int32_t* codes, float* s_a);
 
+/* ------------------------------------------------------------------------
+ * 8-bit linear layers with one scale per token and per output channel.
+ *
+ * soniq_mp_gemm shares an activation scale over the whole batch (C2), so a
+ * token's codes depend on its neighbours.  The calls below take the other
+ * common form: every token (row of A) has its own scale, every output
+ * channel (row of W) its own, all codes are 8 bits, and a token's outputs
+ * depend on nothing but that token.  Operands are plain row-major int8
+ * matrices: soniq_quantize_rows makes both (weights once, offline).
+ *
+ * Rows may start anywhere and have any length; rows whose first byte and
+ * leading dimension are multiples of 16 load fastest.
+ * ---------------------------------------------------------------------- */
+
+/* Element types of the values these calls read and write. */
+enum { SONIQ_F32 = 0, SONIQ_BF16 = 1, SONIQ_F16 = 2 };
+
+/*
+ * soniq_quantize_rows -- symmetric 8-bit codes with one scale per row:
+ *     s[m] = max_k |A[m,k]| / 127,   Q[m,k] = rint(A[m,k] / s[m]),
+ * both divisions fp32, rounded to nearest even (Sec. 3 codec, items 1 and 3
+ * on the symmetric grid).  A row of zeros has scale 0 and codes 0.  A row
+ * that holds an infinity or a NaN has that scale and codes 0, so that its
+ * products are NaN and no other row's are.
+ *   A_dev    device, a_type (SONIQ_F32, SONIQ_BF16 or SONIQ_F16) [M, lda]
+ *   Q_dev    device, int8 [M, ldq]; columns K.. of a row are not written
+ *   s_dev    device, fp32 [M]
+ * M = 0 is allowed and does nothing.  Errors: INVALID_ARGUMENT, UNSUPPORTED
+ * (K > SONIQ_MAX_K, M >= 2^31), HIP.
+ */
+soniq_status soniq_quantize_rows(const void* A_dev, int a_type, int64_t M, int64_t K, int64_t lda,
+                                 int8_t* Q_dev, int64_t ldq, float* s_dev, void* stream);
+
+/*
+ * soniq_i8_gemm -- Y[m,n] = sum_k A[m,k] W[n,k] * s_a[m] * s_w[n] + bias[n].
+ * The sum is exact (int32); the scaling is fp32, in the order
+ * (float(sum) * s_a) * s_w + bias, rounded once to y_type.
+ *   A_dev    device, int8 [M, lda]      s_a_dev  device, fp32 [M]
+ *   W_dev    device, int8 [N, ldw]      s_w_dev  device, fp32 [N]
+ *   bias_dev device, fp32 [N], or NULL
+ *   Y_dev    device, y_type [M, ldy]; columns N.. of a row are not written
+ * M = 0 is allowed and does nothing.  Errors: INVALID_ARGUMENT, UNSUPPORTED
+ * (K > SONIQ_MAX_K, M or N >= 2^31), HIP.
+ */
+soniq_status soniq_i8_gemm(const int8_t* A_dev, int64_t lda, const float* s_a_dev,
+                           const int8_t* W_dev, int64_t ldw, const float* s_w_dev,
+                           const float* bias_dev, int64_t M, int64_t N, int64_t K, void* Y_dev,
+                           int y_type, int64_t ldy, void* stream);
+
+/*
+ * soniq_quantize_i8_gemm -- soniq_quantize_rows(A) then soniq_i8_gemm, with
+ * the codes and scales in the caller's workspace (a few tokens take one
+ * launch).  Results are bit-identical to the two calls.
+ *   work_dev    device, 16-byte aligned, at least the bytes that
+ *               soniq_quantize_i8_gemm_workspace gives for (M, K); holds
+ *               nothing between calls, and calls that may overlap need one
+ *               each
+ * The other arguments and errors are those of the two calls.
+ */
+soniq_status soniq_quantize_i8_gemm(const void* A_dev, int a_type, int64_t lda,
+                                    const int8_t* W_dev, int64_t ldw, const float* s_w_dev,
+                                    const float* bias_dev, int64_t M, int64_t N, int64_t K,
+                                    void* Y_dev, int y_type, int64_t ldy, void* work_dev,
+                                    int64_t work_bytes, void* stream);
+soniq_status soniq_quantize_i8_gemm_workspace(int64_t M, int64_t K, int64_t* bytes);
+
+/* ------------------------------------------------------------------------
+ * Key/value cache in 8- or 4-bit codes, and attention over it: what a
+ * decode step reads beside its weights.
+ *
+ * A cache row is one position of one key/value head: head_dim codes and one
+ * fp32 scale, by the codec of soniq_quantize_rows with 127 or 7 as the
+ * largest code.  Rows live in pages of page_size positions; keys and values
+ * are laid out alike:
+ *     codes   [pages][heads][page_size][head_dim * bits / 8] bytes
+ *     scales  [pages][heads][page_size] fp32
+ * 8-bit codes are int8; 4-bit codes are two's complement, element 2i in the
+ * low half of byte i.  A row stands by itself: moving a position (the
+ * accepted branch of a draft, say) is a copy of its codes and scale.
+ *
+ * A page table, int32 [B, table_ld] of which table_width columns count,
+ * names the page of positions [j * page_size, (j + 1) * page_size) of
+ * sequence b at [b, j].  Tables, lengths and prefix sums are read on the
+ * device.  Entries that name no page (negative, or >= pages) and positions
+ * past the table are well-defined: they are not written, read as zeros, and
+ * no query sees them.
+ *
+ * New tokens come as one ragged batch: rows cu[b] .. cu[b+1]-1 are those of
+ * sequence b (cu_dev: int32 [B + 1], ascending from 0).  Rows from cu[B] on
+ * are ignored, and outputs' rows there are left as they were.
+ *
+ * Supported: head_dim 64, 128, 192, 256; bits 4, 8; pages * heads *
+ * page_size < 2^31; table_width * page_size < 2^31.
+ * ---------------------------------------------------------------------- */
+typedef struct {
+  void* k_dev;        /* codes, 16-byte aligned */
+  float* k_scale_dev;
+  void* v_dev;        /* codes, 16-byte aligned */
+  float* v_scale_dev;
+  int64_t pages;
+  int32_t page_size, heads, head_dim, bits;
+} soniq_kv_cache_t;
+
+/*
+ * soniq_kv_write -- quantizes the keys and values of T new tokens into the
+ * cache: row cu[b] + i goes to position start[b] + i of sequence b.
+ *   K_dev, V_dev   device, type [T, heads, head_dim]; the tokens' and the
+ *                  heads' strides in elements, head_dim contiguous
+ *   start_dev      device, int32 [B]
+ * Pages that two sequences share may be written by one of them in a call.
+ * T = 0 or B = 0 does nothing.  Errors: INVALID_ARGUMENT, UNSUPPORTED, HIP.
+ */
+soniq_status soniq_kv_write(const soniq_kv_cache_t* cache, const void* K_dev,
+                            int64_t k_token_stride, int64_t k_head_stride, const void* V_dev,
+                            int64_t v_token_stride, int64_t v_head_stride, int type, int64_t T,
+                            const int32_t* table_dev, int64_t table_ld, int64_t table_width,
+                            int64_t B, const int32_t* cu_dev, const int32_t* start_dev,
+                            void* stream);
+
+/*
+ * soniq_kv_read -- the values of cached positions (code * scale, rounded
+ * once to `type`): position start[b] + i of sequence b into row cu[b] + i
+ * of K and V [T, heads, head_dim].  Arguments and errors as soniq_kv_write.
+ */
+soniq_status soniq_kv_read(const soniq_kv_cache_t* cache, void* K_dev, int64_t k_token_stride,
+                           int64_t k_head_stride, void* V_dev, int64_t v_token_stride,
+                           int64_t v_head_stride, int type, int64_t T, const int32_t* table_dev,
+                           int64_t table_ld, int64_t table_width, int64_t B,
+                           const int32_t* cu_dev, const int32_t* start_dev, void* stream);
+
+/*
+ * soniq_kv_attention -- attention of new tokens over the cache that already
+ * holds their keys and values:
+ *     O[i] = sum_j softmax_j(scale * q[i] . k[j]) v[j]  over visible j.
+ * Sequence b holds kv_len[b] positions, the last n = cu[b+1] - cu[b] of
+ * them its new tokens'.  Its query i sees every position before
+ * base = kv_len[b] - n, and of the new ones
+ *     without a mask: positions up to its own, base + i;
+ *     with a mask: position base + j where bit j % 64 of word j / 64 of row
+ *     cu[b] + i is set (a tree of drafted tokens: its ancestors and itself).
+ * A query that sees nothing gets zeros (and lse -inf).
+ *   q_dev      device, type SONIQ_BF16 or SONIQ_F16 [T, q_heads, head_dim];
+ *              strides in elements, head_dim contiguous; q_heads a multiple
+ *              of the cache's heads: query head h reads head
+ *              h / (q_heads / heads)
+ *   kv_len_dev device, int32 [B]
+ *   mask_dev   device, uint64 [T, mask_words], or NULL (mask_words then 0);
+ *              tokens past the mask's 64 * mask_words bits are not seen
+ *   max_q      the largest n, at most 256; queries of a sequence from max_q
+ *              on are not computed (their rows are left as they were)
+ *   max_kv     the largest kv_len; only a hint for the split of the work,
+ *              results hold for any lengths
+ *   out_dev    device, type [T, q_heads, head_dim], strides as q's
+ *   lse_dev    device, fp32 [T, q_heads]: log of the softmax's sum, or NULL
+ *   work_dev   device, 16-byte aligned, at least the bytes that
+ *              soniq_kv_attention_workspace gives for the same T, q_heads,
+ *              B, max_q, max_kv; holds nothing between calls, and calls
+ *              that may overlap need one each
+ * T = 0 or B = 0 does nothing.  The same arguments give the same bits on
+ * every call.  Errors: INVALID_ARGUMENT, UNSUPPORTED, HIP.
+ */
+soniq_status soniq_kv_attention(const soniq_kv_cache_t* cache, const void* q_dev,
+                                int64_t q_token_stride, int64_t q_head_stride, int type, int64_t T,
+                                int32_t q_heads, const int32_t* table_dev, int64_t table_ld,
+                                int64_t table_width, int64_t B, const int32_t* cu_dev,
+                                const int32_t* kv_len_dev, const uint64_t* mask_dev,
+                                int32_t mask_words, float scale, int64_t max_q, int64_t max_kv,
+                                void* out_dev, int64_t out_token_stride, int64_t out_head_stride,
+                                float* lse_dev, void* work_dev, int64_t work_bytes, void* stream);
+soniq_status soniq_kv_attention_workspace(const soniq_kv_cache_t* cache, int64_t T,
+                                          int32_t q_heads, int64_t B, int64_t max_q,
+                                          int64_t max_kv, int64_t* bytes);
+
 /*
  * soniq_act_wait_timeouts -- how many workgroups of the single-pass
  * quantizer gave up waiting for the rest of their grid since `act` was

@@ -28,6 +28,9 @@ SONIQ_WPACK_SIGN_NIBBLES = 0x100
 SONIQ_WPACK_F8F6F4 = 0x200
 SONIQ_WPACK_DENSE = 0x400
 SONIQ_MAX_K = 65536
+SONIQ_F32 = 0
+SONIQ_BF16 = 1
+SONIQ_F16 = 2
 
 # Every symbol include/soniq.h declares.
 EXPORTED = [
@@ -42,6 +45,9 @@ EXPORTED = [
     "soniq_weights_destroy",
     "soniq_act_destroy",
     "soniq_last_error",
+    "soniq_quantize_rows", "soniq_i8_gemm", "soniq_quantize_i8_gemm",
+    "soniq_quantize_i8_gemm_workspace",
+    "soniq_kv_write", "soniq_kv_read", "soniq_kv_attention", "soniq_kv_attention_workspace",
 ]
 
 
@@ -61,6 +67,15 @@ class WeightsInfo(ctypes.Structure):
         ("packed_w_bytes_algorithmic", ctypes.c_int64),
         ("act_group_bits", ctypes.c_int32), ("act_scales", ctypes.c_int32),
         ("f8f6f4", ctypes.c_int32), ("dense_w_bytes", ctypes.c_int64),
+    ]
+
+
+class KVCacheStruct(ctypes.Structure):
+    _fields_ = [
+        ("k", ctypes.c_void_p), ("k_scale", ctypes.c_void_p),
+        ("v", ctypes.c_void_p), ("v_scale", ctypes.c_void_p),
+        ("pages", ctypes.c_int64), ("page_size", ctypes.c_int32), ("heads", ctypes.c_int32),
+        ("head_dim", ctypes.c_int32), ("bits", ctypes.c_int32),
     ]
 
 
@@ -116,6 +131,26 @@ def lib() -> ctypes.CDLL:
         L.soniq_act_wait_timeouts.argtypes = [vp, ctypes.POINTER(ctypes.c_uint64)]
         L.soniq_debug_stream_read.restype = st
         L.soniq_debug_stream_read.argtypes = [vp, i64, vp, vp]
+        f32 = ctypes.c_float
+        L.soniq_quantize_rows.restype = st
+        L.soniq_quantize_rows.argtypes = [vp, i32, i64, i64, i64, vp, i64, vp, vp]
+        L.soniq_i8_gemm.restype = st
+        L.soniq_i8_gemm.argtypes = [vp, i64, vp, vp, i64, vp, vp, i64, i64, i64, vp, i32, i64, vp]
+        L.soniq_quantize_i8_gemm.restype = st
+        L.soniq_quantize_i8_gemm.argtypes = [vp, i32, i64, vp, i64, vp, vp, i64, i64, i64, vp, i32, i64,
+                                             vp, i64, vp]
+        L.soniq_quantize_i8_gemm_workspace.restype = st
+        L.soniq_quantize_i8_gemm_workspace.argtypes = [i64, i64, ctypes.POINTER(i64)]
+        rows = [vp, vp, i64, i64, vp, i64, i64, i32, i64, vp, i64, i64, i64, vp, vp, vp]
+        L.soniq_kv_write.restype = st
+        L.soniq_kv_write.argtypes = rows
+        L.soniq_kv_read.restype = st
+        L.soniq_kv_read.argtypes = rows
+        L.soniq_kv_attention.restype = st
+        L.soniq_kv_attention.argtypes = [vp, vp, i64, i64, i32, i64, i32, vp, i64, i64, i64, vp, vp, vp,
+                                         i32, f32, i64, i64, vp, i64, i64, vp, vp, i64, vp]
+        L.soniq_kv_attention_workspace.restype = st
+        L.soniq_kv_attention_workspace.argtypes = [vp, i64, i32, i64, i64, i64, ctypes.POINTER(i64)]
         L.soniq_weights_destroy.restype = None
         L.soniq_weights_destroy.argtypes = [vp]
         L.soniq_act_destroy.restype = None
@@ -467,3 +502,295 @@ def soniq_act_wait_timeouts(act: Activations) -> int:
     n = ctypes.c_uint64(0)
     _check(lib().soniq_act_wait_timeouts(act.handle, ctypes.byref(n)))
     return int(n.value)
+
+
+# ---- 8-bit linear layers, and the quantized key/value cache -----------------
+_TYPES = None
+
+
+def _types():
+    global _TYPES
+    if _TYPES is None:
+        import torch
+        _TYPES = {torch.float32: SONIQ_F32, torch.bfloat16: SONIQ_BF16, torch.float16: SONIQ_F16}
+    return _TYPES
+
+
+def _here(t, what: str, dtype=None, dim=None):
+    """Checks that t is a tensor on the current device (of that type and number
+    of dimensions); the library works on the current device alone."""
+    import torch
+    if not isinstance(t, torch.Tensor) or not t.is_cuda:
+        raise TypeError(f"{what} must be a device tensor")
+    if t.device.index != torch.cuda.current_device():
+        raise ValueError(f"{what} is on {t.device}, the current device is cuda:{torch.cuda.current_device()}")
+    if dtype is not None and t.dtype is not dtype:
+        raise TypeError(f"{what} must be {dtype}")
+    if dim is not None and t.dim() != dim:
+        raise TypeError(f"{what} must have {dim} dimensions")
+
+
+def _rows_of(t, what: str):
+    """Leading dimension of a 2-D tensor with unit column stride (a stride says
+    nothing where there is one row, or one column)."""
+    M, K = t.shape
+    ld, unit = t.stride()
+    if unit != 1 and K > 1:
+        raise TypeError(f"{what} must have unit column stride")
+    if M > 1 and ld < K:
+        raise TypeError(f"{what} has rows that overlap")
+    return ld if M > 1 else max(ld, K)
+
+
+def _type_of(t, what: str) -> int:
+    try:
+        return _types()[t.dtype]
+    except KeyError:
+        raise TypeError(f"{what} must be float32, bfloat16 or float16") from None
+
+
+def soniq_quantize_rows(A, out=None, scales=None, stream=None):
+    """Symmetric 8-bit codes of the rows of A (device float32, bfloat16 or
+    float16 [M, K]) with one scale each: tokens, or the output channels of a
+    weight matrix.  Returns (codes int8 [M, K], scales float32 [M])."""
+    import torch
+    _here(A, "A", dim=2)
+    ta, lda = _type_of(A, "A"), _rows_of(A, "A")
+    M, K = A.shape
+    if out is None:
+        out = torch.empty((M, -(-K // 16) * 16), dtype=torch.int8, device=A.device)[:, :K]
+    _here(out, "out", torch.int8, 2)
+    if tuple(out.shape) != (M, K):
+        raise ValueError("out must have A's shape")
+    if scales is None:
+        scales = torch.empty(M, dtype=torch.float32, device=A.device)
+    _here(scales, "scales", torch.float32, 1)
+    if scales.shape[0] != M or not scales.is_contiguous():
+        raise ValueError("scales must be a contiguous [M] tensor")
+    _check(lib().soniq_quantize_rows(A.data_ptr(), ta, M, K, lda, out.data_ptr(), _rows_of(out, "out"),
+                                     scales.data_ptr(), _stream(stream)))
+    return out, scales
+
+
+def _weights_i8(W, s_w, bias, K, out, M, dtype, device):
+    import torch
+    _here(W, "W", torch.int8, 2)
+    N = W.shape[0]
+    if W.shape[1] != K:
+        raise ValueError("W has the wrong number of input channels")
+    _here(s_w, "s_w", torch.float32, 1)
+    if s_w.shape[0] != N or not s_w.is_contiguous():
+        raise ValueError("s_w must be a contiguous [N] tensor")
+    if bias is not None:
+        _here(bias, "bias", torch.float32, 1)
+        if bias.shape[0] != N or not bias.is_contiguous():
+            raise ValueError("bias must be a contiguous [N] tensor")
+    if out is None:
+        out = torch.empty((M, N), dtype=torch.bfloat16 if dtype is None else dtype, device=device)
+    else:
+        _here(out, "out", dtype, 2)
+        if tuple(out.shape) != (M, N):
+            raise ValueError("out must be [M, N]")
+    return N, out
+
+
+def soniq_i8_gemm(A, s_a, W, s_w, bias=None, out=None, dtype=None, stream=None):
+    """Y = (A W^T) * s_a[:, None] * s_w + bias of int8 codes A [M, K] and
+    W [N, K] with float32 scales per row; Y [M, N] of `dtype` (bfloat16 unless
+    given).  Returns Y."""
+    import torch
+    _here(A, "A", torch.int8, 2)
+    M, K = A.shape
+    _here(s_a, "s_a", torch.float32, 1)
+    if s_a.shape[0] != M or not s_a.is_contiguous():
+        raise ValueError("s_a must be a contiguous [M] tensor")
+    N, out = _weights_i8(W, s_w, bias, K, out, M, dtype, A.device)
+    _check(lib().soniq_i8_gemm(A.data_ptr(), _rows_of(A, "A"), s_a.data_ptr(), W.data_ptr(),
+                               _rows_of(W, "W"), s_w.data_ptr(), None if bias is None else bias.data_ptr(),
+                               M, N, K, out.data_ptr(), _type_of(out, "out"), _rows_of(out, "out"),
+                               _stream(stream)))
+    return out
+
+
+def soniq_quantize_i8_gemm_workspace(M: int, K: int) -> int:
+    n = ctypes.c_int64()
+    _check(lib().soniq_quantize_i8_gemm_workspace(M, K, ctypes.byref(n)))
+    return n.value
+
+
+def soniq_quantize_i8_gemm(A, W, s_w, bias=None, out=None, dtype=None, work=None, stream=None):
+    """soniq_quantize_rows(A), then soniq_i8_gemm with W and s_w, in one call.
+    work: a uint8 device tensor of soniq_quantize_i8_gemm_workspace(M, K)
+    bytes (allocated when None).  Returns Y."""
+    import torch
+    _here(A, "A", dim=2)
+    ta, lda = _type_of(A, "A"), _rows_of(A, "A")
+    M, K = A.shape
+    N, out = _weights_i8(W, s_w, bias, K, out, M, dtype, A.device)
+    if work is None:
+        work = torch.empty(soniq_quantize_i8_gemm_workspace(M, K), dtype=torch.uint8, device=A.device)
+    _here(work, "work", torch.uint8, 1)
+    _check(lib().soniq_quantize_i8_gemm(A.data_ptr(), ta, lda, W.data_ptr(), _rows_of(W, "W"), s_w.data_ptr(),
+                                        None if bias is None else bias.data_ptr(), M, N, K, out.data_ptr(),
+                                        _type_of(out, "out"), _rows_of(out, "out"), work.data_ptr(),
+                                        work.numel(), _stream(stream)))
+    return out
+
+
+class KVCache:
+    """A key/value cache of 8- or 4-bit codes in pages (soniq_kv_cache_t).
+
+    k, v: int8 or uint8 codes [pages, heads, page_size, head_dim * bits / 8];
+    k_scale, v_scale: float32 [pages, heads, page_size]; all contiguous, on
+    one device.  The object keeps the tensors; they stay the caller's to read,
+    copy and move.  KVCache.empty makes them."""
+
+    def __init__(self, k, k_scale, v, v_scale, bits: int = 8):
+        import torch
+        for t, what in ((k, "k"), (v, "v")):
+            _here(t, what, dim=4)
+            if t.dtype not in (torch.int8, torch.uint8) or not t.is_contiguous():
+                raise TypeError(f"{what} must be a contiguous int8 or uint8 tensor")
+        for t, what in ((k_scale, "k_scale"), (v_scale, "v_scale")):
+            _here(t, what, torch.float32, 3)
+            if not t.is_contiguous():
+                raise TypeError(f"{what} must be contiguous")
+        if bits not in (4, 8):
+            raise ValueError("bits must be 4 or 8")
+        if v.shape != k.shape or k_scale.shape != k.shape[:3] or v_scale.shape != k.shape[:3]:
+            raise ValueError("k, v and the scales have different extents")
+        self.k, self.k_scale, self.v, self.v_scale, self.bits = k, k_scale, v, v_scale, bits
+        self.pages, self.heads, self.page_size, width = k.shape
+        self.head_dim = width * 8 // bits
+        self.device = k.device
+        self._c = KVCacheStruct(k.data_ptr(), k_scale.data_ptr(), v.data_ptr(), v_scale.data_ptr(),
+                                self.pages, self.page_size, self.heads, self.head_dim, bits)
+        self._ref = ctypes.addressof(self._c)
+
+    @classmethod
+    def empty(cls, pages: int, page_size: int, heads: int, head_dim: int, bits: int = 8, device=None):
+        """A cache of zeros."""
+        import torch
+        device = torch.device("cuda", torch.cuda.current_device()) if device is None else device
+        codes = lambda: torch.zeros((pages, heads, page_size, head_dim * bits // 8), dtype=torch.int8, device=device)  # noqa: E731
+        scales = lambda: torch.zeros((pages, heads, page_size), dtype=torch.float32, device=device)  # noqa: E731
+        return cls(codes(), scales(), codes(), scales(), bits)
+
+
+def _kv_batch(cache, page_table, cu, lengths, what):
+    import torch
+    if cache.device.index != torch.cuda.current_device():
+        raise ValueError(f"the cache is on {cache.device}, the current device is cuda:{torch.cuda.current_device()}")
+    i32 = torch.int32
+    _here(page_table, "page_table", i32, 2)
+    _here(cu, "cu", i32, 1)
+    _here(lengths, what, i32, 1)
+    B = page_table.shape[0]
+    if cu.shape[0] != B + 1 or lengths.shape[0] != B or not cu.is_contiguous() or not lengths.is_contiguous():
+        raise ValueError(f"cu must be a contiguous [B + 1], {what} a contiguous [B] tensor")
+    return B, page_table.shape[1], _rows_of(page_table, "page_table")
+
+
+def _kv_rows(t, what: str, heads: int, head_dim: int):
+    """Type code and strides of a [T, heads, head_dim] tensor."""
+    _here(t, what, dim=3)
+    if t.shape[1] != heads or t.shape[2] != head_dim:
+        raise ValueError(f"{what} must be [T, {heads}, {head_dim}]")
+    ts, hs, unit = t.stride()
+    if unit != 1:
+        raise TypeError(f"{what} must have unit stride in its last dimension")
+    return _type_of(t, what), ts, hs
+
+
+def soniq_kv_write(cache: KVCache, K, V, page_table, cu, start, stream=None) -> None:
+    """Quantizes new keys and values [T, heads, head_dim] into the cache: row
+    cu[b] + i goes to position start[b] + i of sequence b, whose pages
+    page_table[b] names.  page_table int32 [B, width], cu int32 [B + 1],
+    start int32 [B], all on the device."""
+    B, width, ld = _kv_batch(cache, page_table, cu, start, "start")
+    tk, kts, khs = _kv_rows(K, "K", cache.heads, cache.head_dim)
+    tv, vts, vhs = _kv_rows(V, "V", cache.heads, cache.head_dim)
+    if tk != tv or K.shape[0] != V.shape[0]:
+        raise ValueError("K and V must have one type and one number of tokens")
+    _check(lib().soniq_kv_write(cache._ref, K.data_ptr(), kts, khs, V.data_ptr(), vts, vhs, tk, K.shape[0],
+                                page_table.data_ptr(), ld, width, B, cu.data_ptr(), start.data_ptr(),
+                                _stream(stream)))
+
+
+def soniq_kv_read(cache: KVCache, page_table, cu, start, tokens: int, dtype=None, out=None, stream=None):
+    """The values of cached positions: position start[b] + i of sequence b in
+    row cu[b] + i of K and V [tokens, heads, head_dim] (of `dtype`, bfloat16
+    unless given, or into the pair `out`).  Returns (K, V); rows from cu[B] on
+    are left as they are (out=None: uninitialised)."""
+    import torch
+    B, width, ld = _kv_batch(cache, page_table, cu, start, "start")
+    if out is None:
+        kv = torch.empty((2, tokens, cache.heads, cache.head_dim),
+                         dtype=torch.bfloat16 if dtype is None else dtype, device=cache.device)
+        out = kv[0], kv[1]
+    K, V = out
+    tk, kts, khs = _kv_rows(K, "K", cache.heads, cache.head_dim)
+    tv, vts, vhs = _kv_rows(V, "V", cache.heads, cache.head_dim)
+    if tk != tv or K.shape[0] != tokens or V.shape[0] != tokens or (dtype is not None and K.dtype is not dtype):
+        raise ValueError("K and V must have one type (dtype) and `tokens` rows")
+    _check(lib().soniq_kv_read(cache._ref, K.data_ptr(), kts, khs, V.data_ptr(), vts, vhs, tk, tokens,
+                               page_table.data_ptr(), ld, width, B, cu.data_ptr(), start.data_ptr(),
+                               _stream(stream)))
+    return K, V
+
+
+def soniq_kv_attention_workspace(cache: KVCache, tokens: int, q_heads: int, B: int, max_q: int,
+                                 max_kv: int) -> int:
+    n = ctypes.c_int64()
+    _check(lib().soniq_kv_attention_workspace(cache._ref, tokens, q_heads, B, max_q, max_kv, ctypes.byref(n)))
+    return n.value
+
+
+def soniq_kv_attention(cache: KVCache, q, page_table, cu, kv_len, scale=None, mask=None, max_q=None,
+                       max_kv=None, out=None, lse=None, work=None, stream=None):
+    """Attention of new tokens q [T, q_heads, head_dim] (bfloat16 or float16)
+    over the cache that already holds their keys and values.  Sequence b has
+    kv_len[b] positions, the last cu[b+1] - cu[b] of them its new tokens'.
+    mask (int64 [T, words]): bit j % 64 of word j / 64 of a row says whether
+    that token sees new token j of its sequence; None: each sees the new ones
+    up to itself.  scale: 1 / sqrt(head_dim) unless given.  max_q: the most
+    new tokens of a sequence (T unless given; at most 256); max_kv: the
+    longest kv_len, a hint.  lse: a float32 [T, q_heads] tensor to fill.
+    work: a uint8 device tensor of soniq_kv_attention_workspace(...) bytes
+    (allocated when None).  Returns out (like q)."""
+    import torch
+    B, width, ld = _kv_batch(cache, page_table, cu, kv_len, "kv_len")
+    if q.dim() != 3:
+        raise TypeError("q must have 3 dimensions")
+    T, heads = q.shape[0], q.shape[1]
+    tq, qts, qhs = _kv_rows(q, "q", heads, cache.head_dim)
+    if out is None:
+        out = torch.empty((T, heads, cache.head_dim), dtype=q.dtype, device=q.device)
+    to, ots, ohs = _kv_rows(out, "out", heads, cache.head_dim)
+    if to != tq or out.shape[0] != T:
+        raise ValueError("out must have q's shape and type")
+    words = 0
+    if mask is not None:
+        _here(mask, "mask", torch.int64, 2)
+        if mask.shape[0] != T or not mask.is_contiguous():
+            raise ValueError("mask must be a contiguous [T, words] tensor")
+        words = mask.shape[1]
+    if lse is not None:
+        _here(lse, "lse", torch.float32, 2)
+        if tuple(lse.shape) != (T, heads) or not lse.is_contiguous():
+            raise ValueError("lse must be a contiguous [T, q_heads] tensor")
+    if max_q is None:
+        max_q = max(T, 1)
+    if max_kv is None:
+        max_kv = width * cache.page_size
+    if work is None:
+        work = torch.empty(soniq_kv_attention_workspace(cache, T, heads, B, max_q, max_kv), dtype=torch.uint8,
+                           device=q.device)
+    _here(work, "work", torch.uint8, 1)
+    _check(lib().soniq_kv_attention(cache._ref, q.data_ptr(), qts, qhs, tq, T, heads, page_table.data_ptr(), ld,
+                                    width, B, cu.data_ptr(), kv_len.data_ptr(),
+                                    None if mask is None else mask.data_ptr(), words,
+                                    cache.head_dim ** -0.5 if scale is None else scale, max_q, max_kv,
+                                    out.data_ptr(), ots, ohs, None if lse is None else lse.data_ptr(),
+                                    work.data_ptr(), work.numel(), _stream(stream)))
+    return out

@@ -35,13 +35,26 @@ namespace {
 
 thread_local std::string g_err;
 
-soniq_status fail(soniq_status st, const char* fmt, ...) {
+}  // namespace
+
+namespace soniq {
+
+int set_error(int st, const char* fmt, va_list ap) {
   char buf[512];
+  vsnprintf(buf, sizeof buf, fmt, ap);
+  g_err = buf;
+  return st;
+}
+
+}  // namespace soniq
+
+namespace {
+
+soniq_status fail(soniq_status st, const char* fmt, ...) {
   va_list ap;
   va_start(ap, fmt);
-  vsnprintf(buf, sizeof buf, fmt, ap);
+  set_error(st, fmt, ap);
   va_end(ap);
-  g_err = buf;
   return st;
 }
 

@@ -27,9 +27,14 @@
 #pragma once
 #include <hip/hip_runtime.h>
 
+#include <cstdarg>
 #include <cstdint>
 
 namespace soniq {
+
+// Records the message of a failed call for soniq_last_error() (this
+// thread's); returns `st`, a soniq_status.
+int set_error(int st, const char* fmt, va_list ap);
 
 constexpr int kGran = 64;     // channels per granule
 constexpr int kBlk = 16;      // rows per block

@@ -1,0 +1,169 @@
+"""8-bit linear layers with one scale per token and per output channel:
+codes, scales and outputs equal the oracle's bit for bit (the order of the
+fp32 scaling is fixed, the sums are exact), at sizes on and off every tile,
+for tokens that start anywhere and for rows of zeros, infinities and NaN."""
+import numpy as np
+import pytest
+import torch
+
+import paper_2311_14114_amd as sq
+from oracle import serve
+
+pytestmark = pytest.mark.gpu
+
+TYPES = {"fp32": torch.float32, "bf16": torch.bfloat16, "fp16": torch.float16}
+
+
+def _tokens(M, K, dtype, gap=0, seed=0, offset=0):
+    """[M, K] tokens inside a wider buffer, `offset` elements from its start."""
+    g = torch.Generator().manual_seed(seed + M * 7 + K)
+    x = torch.randn((M, K + gap), generator=g)
+    x[:, torch.rand(K + gap, generator=g) < 0.01] *= 20
+    flat = torch.zeros(M * (K + gap) + offset, dtype=TYPES[dtype], device="cuda")
+    flat[offset:] = x.to(TYPES[dtype]).flatten().cuda()
+    return flat[offset:].view(M, K + gap)[:, :K]
+
+
+def _codes(M, K, seed, ld=None, offset=0):
+    r = np.random.default_rng(seed)
+    ld = K if ld is None else ld
+    x = r.integers(-128, 128, (M, ld)).astype(np.int8)
+    flat = torch.zeros(M * ld + offset, dtype=torch.int8, device="cuda")
+    flat[offset:] = torch.from_numpy(x).flatten().cuda()
+    return flat[offset:].view(M, ld)[:, :K], x[:, :K]
+
+
+def _same(got, want):
+    """Bit for bit, with any NaN equal to any other."""
+    got, want = got.cpu(), want.cpu()
+    assert got.shape == want.shape and got.dtype == want.dtype
+    nan = torch.isnan(want) if want.is_floating_point() else torch.zeros(want.shape, dtype=torch.bool)
+    if want.is_floating_point():
+        assert torch.equal(torch.isnan(got), nan)
+    assert torch.equal(got[~nan], want[~nan])
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16", "fp16"])
+@pytest.mark.parametrize("M,K,gap,offset", [
+    (1, 1, 0, 0), (1, 64, 0, 0), (3, 100, 5, 1), (5, 4091, 3, 3), (2, 4096, 0, 0), (33, 768, 0, 2),
+    (700, 130, 1, 0), (9, 8192, 8, 0), (2, 16389, 0, 0), (1, 65536, 0, 1), (4100, 16, 0, 0)])
+def test_quantize_rows(M, K, gap, offset, dtype):
+    A = _tokens(M, K, dtype, gap, offset=offset)
+    print(f"[gpu] quantize_rows {M}x{K} {dtype}", flush=True)
+    back = torch.full((M, K + 7), 99, dtype=torch.int8, device="cuda")
+    Q, s = sq.soniq_quantize_rows(A, out=back[:, :K])
+    q, sc = serve.quantize_rows(A.float().cpu().numpy())
+    _same(Q, torch.from_numpy(q))
+    _same(s, torch.from_numpy(sc))
+    assert bool((back[:, K:] == 99).all())          # columns past K are left alone
+
+
+def test_quantize_rows_special():
+    """Rows of zeros, ties, the smallest and largest values, infinities and
+    NaN; each row by itself."""
+    K = 300
+    A = np.random.default_rng(0).standard_normal((10, K)).astype(np.float32)
+    A[1] = 0
+    A[2, 7] = np.inf
+    A[3, 299] = np.nan
+    A[4, 0] = -np.inf
+    A[5] = 2.0**-149 * np.arange(K)
+    A[6] *= 1e38 / np.abs(A[6]).max()
+    A[7] = np.repeat([127, 0.5, 1.5, -2.5, 63.5, -0.5], 50)
+    A[8] = -0.0
+    A[9] = np.where(np.arange(K) == 4, np.nan, np.inf)
+    Q, s = sq.soniq_quantize_rows(torch.from_numpy(A).cuda())
+    q, sc = serve.quantize_rows(A)
+    _same(Q, torch.from_numpy(q))
+    _same(s, torch.from_numpy(sc))
+    assert torch.isnan(s[3]) and torch.isinf(s[2]) and s[1] == 0
+
+
+SHAPES = [  # M, N, K
+    (1, 1, 1), (1, 16, 64), (1, 4096, 4096), (1, 100, 16389), (2, 130, 256), (3, 1030, 4091), (4, 64, 65536),
+    (5, 11, 127), (7, 515, 512), (8, 4096, 1024), (9, 300, 640), (16, 128, 128), (17, 17, 17), (24, 1100, 96),
+    (33, 4099, 257), (40, 256, 4096), (48, 33, 8192), (63, 65, 63), (64, 64, 64), (65, 129, 191), (100, 768, 768),
+    (128, 128, 4096), (129, 257, 385), (200, 2304, 768), (256, 256, 256), (257, 511, 1000), (301, 199, 4091),
+    (513, 1025, 129), (1000, 300, 2048), (2049, 140, 320), (1, 70000, 64), (4097, 65, 64), (512, 2560, 1152)]
+
+
+@pytest.mark.parametrize("M,N,K", SHAPES, ids=lambda v: str(v))
+@pytest.mark.parametrize("form", ["plain", "odd"])
+def test_i8_gemm(M, N, K, form):
+    """Codes of the whole int8 range; `odd`: leading dimensions and starts
+    that no load width divides, a bias, fp16 into a wider output."""
+    odd = form == "odd"
+    A, a = _codes(M, K, 1, K + 5 if odd else K, 3 if odd else 0)
+    W, w = _codes(N, K, 2, K + 9 if odd else K, 1 if odd else 0)
+    r = np.random.default_rng(M + N + K)
+    sa = np.exp(r.standard_normal(M)).astype(np.float32)
+    sw = (np.exp(r.standard_normal(N)) / 1e3).astype(np.float32)
+    bias = r.standard_normal(N).astype(np.float32) if odd else None
+    dt = torch.float16 if odd else torch.bfloat16
+    if odd:
+        sa /= 64 * np.sqrt(K)                        # outputs inside fp16's range
+    print(f"[gpu] i8_gemm {M}x{N}x{K} {form}", flush=True)
+    wide = torch.full((M, N + 3), 7.0, dtype=dt, device="cuda")
+    cuda = lambda x: None if x is None else torch.from_numpy(x).cuda()
+    Y = sq.soniq_i8_gemm(A, cuda(sa), W, cuda(sw), bias=cuda(bias), out=wide[:, :N])
+    want = torch.from_numpy(serve.i8_gemm(a, sa, w, sw, bias))
+    _same(Y, want.to(dt))
+    assert bool((wide[:, N:] == 7.0).all())
+    Y32 = sq.soniq_i8_gemm(A, cuda(sa), W, cuda(sw), bias=cuda(bias), dtype=torch.float32)
+    _same(Y32, want)
+
+
+@pytest.mark.parametrize("M,N,K,gap", [(1, 4096, 4096, 0), (1, 33, 100, 3), (2, 1100, 768, 0), (3, 100, 8191, 1),
+                                       (4, 256, 2048, 0), (5, 64, 512, 0), (8, 130, 11008, 0), (9, 40, 65, 0),
+                                       (40, 300, 1024, 5), (300, 512, 640, 0), (1, 24, 65536, 0)])
+@pytest.mark.parametrize("dtype", ["fp32", "bf16", "fp16"])
+def test_quantize_i8_gemm_equals_the_two_calls(M, N, K, gap, dtype):
+    A = _tokens(M, K, dtype, gap)
+    A[M // 2] *= 0                                   # a token of zeros among the others
+    W, w = _codes(N, K, 5)
+    sw = torch.rand(N, device="cuda") / 100
+    print(f"[gpu] quantize_i8_gemm {M}x{N}x{K} {dtype}", flush=True)
+    Y = sq.soniq_quantize_i8_gemm(A, W, sw, dtype=TYPES[dtype])
+    q, s = sq.soniq_quantize_rows(A)
+    _same(Y, sq.soniq_i8_gemm(q, s, W, sw, dtype=TYPES[dtype]))
+    qo, so = serve.quantize_rows(A.float().cpu().numpy())
+    _same(Y, torch.from_numpy(serve.i8_gemm(qo, so, w, sw.cpu().numpy())).to(TYPES[dtype]))
+
+
+@pytest.mark.parametrize("M", [1, 3, 40, 300])
+def test_a_bad_token_spoils_itself_alone(M):
+    A = _tokens(M, 512, "bf16", seed=3)
+    clean = A.clone()
+    A[0, 100], A[M // 2, 3] = float("nan"), float("inf")
+    W, _ = _codes(200, 512, 5)
+    sw = torch.rand(200, device="cuda") / 100
+    Y, ref = sq.soniq_quantize_i8_gemm(A, W, sw), sq.soniq_quantize_i8_gemm(clean, W, sw)
+    bad = torch.zeros(M, dtype=torch.bool, device="cuda")
+    bad[0] = bad[M // 2] = True
+    assert bool(torch.isnan(Y[bad].float()).all())
+    assert torch.equal(Y[~bad], ref[~bad])
+
+
+def test_no_tokens():
+    W, _ = _codes(20, 64, 5)
+    sw = torch.rand(20, device="cuda")
+    assert sq.soniq_quantize_i8_gemm(torch.empty((0, 64), device="cuda"), W, sw).shape == (0, 20)
+
+
+def test_streams_and_shared_weights():
+    """Two streams at once, each with its own workspace, on one weight matrix."""
+    W, w = _codes(1024, 1024, 5)
+    sw = torch.rand(1024, device="cuda") / 100
+    xs = [_tokens(M, 1024, "bf16", seed=M) for M in (1, 200)]
+    want = [sq.soniq_quantize_i8_gemm(x, W, sw) for x in xs]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    got = [[], []]
+    for _ in range(4):
+        for k, st in enumerate(streams):
+            with torch.cuda.stream(st):
+                got[k].append(sq.soniq_quantize_i8_gemm(xs[k], W, sw))
+    torch.cuda.synchronize()
+    for k in (0, 1):
+        for y in got[k]:
+            assert torch.equal(y, want[k])
