@@ -2,6 +2,8 @@
 #include "soniq_serve.h"
 #include "soniq_values.h"
 
+#include <algorithm>
+
 namespace soniq {
 namespace {
 
@@ -57,66 +59,560 @@ __global__ __launch_bounds__(64) void k_kv_copy(KvCopy c) {
   }
 }
 
-// Whether new position j is visible to new query i.
-__device__ __forceinline__ bool sees(const KvAttend& a, int64_t t, int i, int j) {
-  if (!a.mask) return j <= i;
-  return j < 64 * a.mask_words && (a.mask[t * a.mask_words + j / 64] >> (j % 64)) & 1;
+// ---------------------------------------------------------- attention --
+// One workgroup takes 16 * R query rows (new tokens times the heads that
+// share a key/value head) of one sequence and key/value head over one part
+// of its positions; four waves take 32 positions each in turn, keep their
+// own running softmax, and meet at the end.  Parts meet in k_kv_join.
+//
+// Everything stays transposed, so that no operand crosses lanes: with
+// kb = lane / 16 and c = lane % 16,
+//   S^T = K Q^T  (v_mfma_f32_16x16x32_f16, rows = positions): lane holds the
+//         scores of query row c and of positions 4 kb + i and 16 + 4 kb + i;
+//   O^T = V^T P^T: those same eight positions, in that order, are the lane's
+//         eight k elements, so P goes from the scores' registers into the
+//         product; the V operand is 8 positions of one element d, and a lane
+//         that loads elements [c * D/16, (c + 1) * D/16) of its eight rows
+//         holds D/16 such operands, a byte permute away.
+// K and V go from memory to registers; LDS holds the queries' fragments and
+// each position's cache row and scales.
+//
+// Codes become fp16 exactly: a code moved to unsigned, u, is read as the
+// fp16 subnormal u * 2^-24, and one packed fma makes it (u - zero) * 2^-9.
+// Queries are scaled by a power of two per row to use fp16's whole range
+// (bf16 queries are exact in it down to 2^-22 of the row's largest element).
+//
+// Softmax of row r over the positions so far, all in fp32:
+//   m  a value near the largest score (base 2), l = sum exp2(s - m);
+//   w  = exp2(s - m) * s_v / sg, the weight rounded to fp16 for the product,
+//   sg = a value near the largest exp2(s - m) * s_v, so that a weight is off
+//        by at most half a step of fp16 whatever the V scales' range.
+// The accumulators hold O / sg.  m and sg move only when a new value passes
+// them by 2^6 or 2^8 (fp16 has room), so rescaling is rare; a new m scales
+// l and sg alone.
+typedef _Float16 h2 __attribute__((ext_vector_type(2)));
+typedef _Float16 h8 __attribute__((ext_vector_type(8)));
+typedef float f4 __attribute__((ext_vector_type(4)));
+
+constexpr int kSub = 1024;     // positions whose rows and scales LDS holds at a time
+constexpr float kSgMin = 0x1p-120f;
+
+// Barrier for LDS alone: loads from memory stay in flight.
+__device__ __forceinline__ void lds_barrier() {
+  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup", "local");
+  __builtin_amdgcn_s_barrier();
+  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
 }
 
-// One workgroup per (sequence, query, head): 256 positions at a time, one
-// per thread, then the outputs of the chunk, one element per thread.
-template <int TYPE>
-__global__ __launch_bounds__(256) void k_kv_attend(KvAttend a) {
-  typedef typename Value<TYPE>::T T;
-  __shared__ float q[256], p[256];
-  __shared__ int32_t rows[256];
-  __shared__ float red[8];
-  const int i = blockIdx.x, hq = blockIdx.y, b = blockIdx.z, tid = threadIdx.x;
-  const int D = a.dims.head_dim, bits = a.dims.bits, rb = D * bits / 8;
-  const KvSpan sp = kv_span(a.cu[b], a.cu[b + 1], a.T);
-  if (i >= sp.count) return;
-  const int64_t t = sp.first + i;
-  const int len = kv_length(a.table, a.dims, a.kv_len[b]);
-  const int64_t base = (int64_t)a.kv_len[b] - sp.count;
-  const int h = hq / a.group;
-  if (tid < D) q[tid] = Value<TYPE>::load(static_cast<const T*>(a.q)[t * a.q_ts + hq * a.q_hs + tid]);
-  float m = -INFINITY, l = 0.0f, o = 0.0f;
-  for (int j0 = 0; j0 < len; j0 += 256) {
-    __syncthreads();
-    const int j = j0 + tid;
-    float s = -INFINITY;
-    int32_t row = j < len ? kv_row(a.table, a.dims, b, j) : -1;
-    if (row >= 0 && (j < base || sees(a, t, i, (int)(j - base)))) {
-      row += h * a.dims.page_size;
-      float z = 0.0f;
-      for (int d = 0; d < D; ++d) z = fmaf(q[d], (float)code_at(a.k + (int64_t)row * rb, d, bits), z);
-      s = z * a.ks[row] * a.scale;
-    } else {
-      row = -1;
+// Over the four lanes that share c: the same result in each.
+__device__ __forceinline__ float quad_max(float x) {
+  const uint32_t u = __float_as_uint(x);
+  const auto a = __builtin_amdgcn_permlane16_swap(u, u, false, false);
+  x = fmaxf(__uint_as_float(a[0]), __uint_as_float(a[1]));
+  const uint32_t v = __float_as_uint(x);
+  const auto b = __builtin_amdgcn_permlane32_swap(v, v, false, false);
+  return fmaxf(__uint_as_float(b[0]), __uint_as_float(b[1]));
+}
+__device__ __forceinline__ float quad_sum(float x) {
+  const uint32_t u = __float_as_uint(x);
+  const auto a = __builtin_amdgcn_permlane16_swap(u, u, false, false);
+  x = __uint_as_float(a[0]) + __uint_as_float(a[1]);
+  const uint32_t v = __float_as_uint(x);
+  const auto b = __builtin_amdgcn_permlane32_swap(v, v, false, false);
+  return __uint_as_float(b[0]) + __uint_as_float(b[1]);
+}
+
+template <int BITS>
+__device__ __forceinline__ h2 to_half(uint32_t u16pair) {
+  const h2 x = __builtin_bit_cast(h2, u16pair);
+  const _Float16 z = BITS == 8 ? (_Float16)-0.25f : (_Float16)-0x1p-6f;
+  return __builtin_elementwise_fma(x, h2{(_Float16)32768.0f, (_Float16)32768.0f}, h2{z, z});
+}
+
+// Eight K codes as an operand: from two words of 8-bit codes in order, or
+// from one word of 4-bit codes in the order 0 4 1 5 2 6 3 7.
+template <int BITS>
+__device__ __forceinline__ h8 k_operand(const uint32_t* w) {
+  union { h2 p[4]; h8 v; } r;
+  if constexpr (BITS == 8) {
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const uint32_t u = w[i] ^ 0x80808080u;
+      r.p[2 * i] = to_half<8>(__builtin_amdgcn_perm(u, u, 0x0c010c00u));
+      r.p[2 * i + 1] = to_half<8>(__builtin_amdgcn_perm(u, u, 0x0c030c02u));
     }
-    float mx = s;
-    for (int x = 32; x; x >>= 1) mx = fmaxf(mx, __shfl_xor(mx, x));
-    if (tid % 64 == 0) red[tid / 64] = mx;
-    __syncthreads();
-    mx = fmaxf(fmaxf(red[0], red[1]), fmaxf(red[2], red[3]));
-    const float mn = fmaxf(m, mx), al = mn == -INFINITY ? 1.0f : expf(m - mn);
-    const float e = row >= 0 ? expf(s - mn) : 0.0f;
-    float sum = e;
-    for (int x = 32; x; x >>= 1) sum += __shfl_xor(sum, x);
-    if (tid % 64 == 0) red[4 + tid / 64] = sum;
-    p[tid] = row >= 0 ? e * a.vs[row] : 0.0f;
-    rows[tid] = row;
-    __syncthreads();
-    l = l * al + (red[4] + red[5] + red[6] + red[7]);
-    o *= al;
-    m = mn;
-    if (tid < D)
-      for (int x = 0; x < 256; ++x)
-        if (rows[x] >= 0) o = fmaf(p[x], (float)code_at(a.v + (int64_t)rows[x] * rb, tid, bits), o);
+  } else {
+    const uint32_t u = w[0] ^ 0x88888888u;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) r.p[i] = to_half<4>((u >> (4 * i)) & 0x000F000Fu);
   }
-  if (tid < D)
-    static_cast<T*>(a.out)[t * a.o_ts + hq * a.o_hs + tid] = Value<TYPE>::store(l == 0.0f ? 0.0f : o / l);
-  if (tid == 0 && a.lse) a.lse[t * a.q_heads + hq] = l == 0.0f ? -INFINITY : m + logf(l);
+  return r.v;
+}
+// Where element i of a group of eight goes in that operand.
+template <int BITS>
+__device__ __forceinline__ constexpr int k_order(int i) {
+  return BITS == 8 ? i : i < 4 ? 2 * i : 2 * (i - 4) + 1;
+}
+
+// Bytes of a lane's share of a row, loaded in the widest pieces.
+template <int BYTES>
+struct Raw {
+  uint32_t w[(BYTES + 3) / 4];
+  __device__ __forceinline__ void load(const uint8_t* p) {
+    if constexpr (BYTES == 2) {
+      w[0] = *reinterpret_cast<const uint16_t*>(p);
+    } else if constexpr (BYTES == 6) {
+      struct __attribute__((packed, aligned(2))) P { uint32_t a; uint16_t b; };
+      const P x = *reinterpret_cast<const P*>(p);
+      w[0] = x.a;
+      w[1] = x.b;
+    } else {
+#pragma unroll
+      for (int i = 0; i < BYTES / 16; ++i) {
+        const uint4 x = *reinterpret_cast<const uint4*>(p + 16 * i);
+        w[4 * i] = x.x, w[4 * i + 1] = x.y, w[4 * i + 2] = x.z, w[4 * i + 3] = x.w;
+      }
+      constexpr int r = BYTES % 16, o = BYTES / 16 * 4;
+      if constexpr (r == 4) w[o] = *reinterpret_cast<const uint32_t*>(p + 4 * o);
+      if constexpr (r == 8) {
+        const uint2 x = *reinterpret_cast<const uint2*>(p + 4 * o);
+        w[o] = x.x, w[o + 1] = x.y;
+      }
+      if constexpr (r == 12) {
+        const uint3 x = *reinterpret_cast<const uint3*>(p + 4 * o);
+        w[o] = x.x, w[o + 1] = x.y, w[o + 2] = x.z;
+      }
+    }
+  }
+};
+
+// Which of the 32 positions from new position j0 on (negative: older ones)
+// new query i of ragged row t sees.
+__device__ __forceinline__ uint32_t seen_bits(const KvAttend& a, int64_t t, int i, int64_t j0) {
+  if (j0 <= -32) return ~0u;
+  const uint32_t old = j0 < 0 ? (1u << -j0) - 1u : 0u;
+  if (!a.mask) {
+    const int64_t n = i - j0 + 1;
+    return n >= 32 ? ~0u : n <= 0 ? 0u : (1u << n) - 1u;
+  }
+  const uint64_t* w = a.mask + t * a.mask_words;
+  if (j0 < 0) return old | (uint32_t)(w[0] << -j0);
+  const int64_t x = j0 / 64;
+  const int sh = (int)(j0 % 64);
+  if (x >= a.mask_words) return 0u;
+  uint64_t v = w[x] >> sh;
+  if (sh > 32 && x + 1 < a.mask_words) v |= w[x + 1] << (64 - sh);
+  return (uint32_t)v;
+}
+
+// How a launch is cut: parts of at least `chunk` positions each.
+struct KvSplit {
+  int R;      // 16-row tiles a workgroup
+  int RB;     // workgroups over the rows
+  int parts;
+  int chunk;
+};
+
+// The positions of one part: [first, first + count).  A sequence longer than
+// the host was told takes longer parts.
+struct KvPart {
+  int first, count, used;  // used: parts of this sequence that hold positions
+};
+__device__ __forceinline__ KvPart part_of(int len, int part, int parts, int chunk) {
+  int64_t c = ((int64_t)len + parts - 1) / parts;
+  c = (c + 127) & ~(int64_t)127;
+  c = c > chunk ? c : chunk;
+  const int64_t first = part * c;
+  const int count = first >= len ? 0 : (int)min(c, len - first);
+  return {(int)first, count, (int)((len + c - 1) / c)};
+}
+
+template <int D, int R>
+struct KvLds {
+  int32_t row[kSub];
+  float ks[kSub], vs[kSub];
+  uint32_t valid[kSub / 32];
+  h8 q[R][D / 32][64];
+  float qf[16 * R];
+};
+
+__device__ __forceinline__ float q_value(const void* p, int64_t i, int type) {
+  return type == SONIQ_BF16 ? bf16_value(static_cast<const uint16_t*>(p)[i])
+                            : (float)static_cast<const _Float16*>(p)[i];
+}
+
+template <int D, int BITS, int R>
+__global__ __launch_bounds__(256, 2) void k_kv_attend(KvAttend a, KvSplit sp) {
+  constexpr int RB = D * BITS / 8;   // bytes of a cache row
+  constexpr int KB = RB / 4, VB = RB / 16;
+  constexpr int NK = D / 32;         // products over d
+  constexpr int DB = D / 16;         // elements of d a lane holds, and V operands
+  constexpr int OP = D + 4;          // pitch of the outputs in LDS
+  constexpr size_t kLdsLoop = sizeof(KvLds<D, R>), kLdsOut = (size_t)4 * 16 * OP * 4 + 4 * 16 * 8 + 64;
+  __shared__ __align__(16) uint8_t lds_bytes[kLdsLoop > kLdsOut ? kLdsLoop : kLdsOut];
+  KvLds<D, R>& L = *reinterpret_cast<KvLds<D, R>*>(lds_bytes);
+
+  // workgroups of the same positions go to one XCD, one after the other
+  const int H = a.dims.heads, G = a.group;
+  int rb, u;
+  {
+    const uint32_t id = blockIdx.x, x = id / 8;
+    rb = (int)(x % sp.RB);
+    u = (int)(x / sp.RB) * 8 + (int)(id % 8);
+  }
+  const int h = u % H, bp = u / H, part = bp % sp.parts, b = bp / sp.parts;
+  if (b >= a.table.B) return;
+  const KvSpan span = kv_span(a.cu[b], a.cu[b + 1], a.T);
+  const int nq = min(span.count, a.max_q);
+  const int len = kv_length(a.table, a.dims, a.kv_len[b]);
+  const int64_t base = (int64_t)a.kv_len[b] - span.count;
+  const int row0 = rb * 16 * R, rows = min(nq * G - row0, 16 * R);
+  const KvPart pt = part_of(len, part, sp.parts, sp.chunk);
+  if (rows <= 0 || (part > 0 && pt.count == 0)) return;
+
+  const int tid = threadIdx.x, lane = tid % 64, wave = tid / 64, c = lane % 16, kb = lane / 16;
+
+  // ---- queries: scaled to fp16, in operand order
+  {
+    // threads a row: a power of two that leaves each a multiple of 8 elements
+    constexpr int kMost = D % 128 == 0 ? 16 : 8, TPR = 16 / R < kMost ? 16 / R : kMost;
+    constexpr int PER = D / TPR;
+    if (tid < 16 * R * TPR) {
+      const int r = tid / TPR, d0 = tid % TPR * PER;
+      float x[PER];
+      uint32_t mx = 0;
+      if (r < rows) {
+        const int64_t t = span.first + (row0 + r) / G;
+        const int64_t at = t * a.q_ts + ((int64_t)h * G + (row0 + r) % G) * a.q_hs + d0;
+#pragma unroll
+        for (int i = 0; i < PER; ++i) x[i] = q_value(a.q, at + i, a.type);
+      } else {
+#pragma unroll
+        for (int i = 0; i < PER; ++i) x[i] = 0.0f;
+      }
+#pragma unroll
+      for (int i = 0; i < PER; ++i) mx = max(mx, __float_as_uint(x[i]) & 0x7FFFFFFFu);
+#pragma unroll
+      for (int o = 1; o < TPR; o *= 2) mx = max(mx, (uint32_t)__shfl_xor((int)mx, o));
+      // largest element to [2^14, 2^15); rows of zeros, infinities or NaN as they are
+      int e = (int)(mx >> 23) - 127 - 14;
+      e = mx >= 0x7F800000u || mx == 0 ? 0 : max(e, -100);
+      const float down = __uint_as_float((uint32_t)(127 - e) << 23);
+      if (tid % TPR == 0) L.qf[r] = __uint_as_float((uint32_t)(127 + e) << 23) * 512.0f * (a.scale * 1.44269504f);
+#pragma unroll
+      for (int g = 0; g < PER / 8; ++g) {
+        h8 v;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[k_order<BITS>(i)] = (_Float16)(x[8 * g + i] * down);
+        const int d = d0 + 8 * g;
+        L.q[r / 16][d % (D / 4) / 8][d / (D / 4) * 16 + r % 16] = v;
+      }
+    }
+  }
+
+  // query of this lane's row in each tile (masked tiles ask)
+  f4 O[R][DB];
+  float m[R], l[R], sg[R], inv[R];
+#pragma unroll
+  for (int rt = 0; rt < R; ++rt) {
+#pragma unroll
+    for (int j = 0; j < DB; ++j) O[rt][j] = f4{0.0f, 0.0f, 0.0f, 0.0f};
+    m[rt] = -INFINITY, l[rt] = 0.0f, sg[rt] = 0.0f, inv[rt] = 0.0f;
+  }
+
+  const uint8_t* kp = a.k + kb * KB;
+  const uint8_t* vp = a.v + c * VB;
+  Raw<KB> kr[2];
+  Raw<VB> vr[8];
+  auto load_k = [&](int st) {
+#pragma unroll
+    for (int t = 0; t < 2; ++t) kr[t].load(kp + (int64_t)L.row[st * 32 + 16 * t + c] * RB);
+  };
+  auto load_v = [&](int st) {
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+      const int4 x = *reinterpret_cast<const int4*>(&L.row[st * 32 + 16 * t + 4 * kb]);
+      vr[4 * t].load(vp + (int64_t)x.x * RB);
+      vr[4 * t + 1].load(vp + (int64_t)x.y * RB);
+      vr[4 * t + 2].load(vp + (int64_t)x.z * RB);
+      vr[4 * t + 3].load(vp + (int64_t)x.w * RB);
+    }
+  };
+
+  for (int s0 = 0; s0 < pt.count; s0 += kSub) {
+    const int n = min(pt.count - s0, kSub), nst = (n + 31) / 32, p0 = pt.first + s0;
+    if (s0) lds_barrier();  // the last sub-part's rows and scales have been read
+    float kreg[kSub / 256], vreg[kSub / 256];
+#pragma unroll
+    for (int k = 0; k < kSub / 256; ++k) {
+      const int x = tid + 256 * k;
+      kreg[k] = vreg[k] = 0.0f;
+      if (256 * k < n) {
+        int32_t row = x < n ? kv_row(a.table, a.dims, b, p0 + x) : -1;
+        const uint64_t there = __ballot(row >= 0);
+        if (lane == 0) L.valid[x / 32] = (uint32_t)there;
+        if (lane == 32) L.valid[x / 32] = (uint32_t)(there >> 32);
+        row = row < 0 ? 0 : row + h * a.dims.page_size;
+        L.row[x] = row;
+        kreg[k] = a.ks[row], vreg[k] = a.vs[row];
+      }
+    }
+    lds_barrier();
+    if (wave < nst) {
+      load_k(wave);
+      load_v(wave);
+    }
+#pragma unroll
+    for (int k = 0; k < kSub / 256; ++k)
+      if (256 * k < n) L.ks[tid + 256 * k] = kreg[k], L.vs[tid + 256 * k] = vreg[k];
+    lds_barrier();
+
+    for (int st = wave; st < nst; st += 4) {
+      const bool more = st + 4 < nst;
+      f4 S[R][2];
+#pragma unroll
+      for (int rt = 0; rt < R; ++rt) S[rt][0] = S[rt][1] = f4{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+      for (int s = 0; s < NK; ++s) {
+        const h8 k0 = k_operand<BITS>(&kr[0].w[s * (BITS == 8 ? 2 : 1)]);
+        const h8 k1 = k_operand<BITS>(&kr[1].w[s * (BITS == 8 ? 2 : 1)]);
+#pragma unroll
+        for (int rt = 0; rt < R; ++rt) {
+          const h8 q = L.q[rt][s][lane];
+          S[rt][0] = __builtin_amdgcn_mfma_f32_16x16x32_f16(k0, q, S[rt][0], 0, 0, 0);
+          S[rt][1] = __builtin_amdgcn_mfma_f32_16x16x32_f16(k1, q, S[rt][1], 0, 0, 0);
+        }
+      }
+      if (more) load_k(st + 4);
+
+      const f4 ks0 = *reinterpret_cast<const f4*>(&L.ks[st * 32 + 4 * kb]);
+      const f4 ks1 = *reinterpret_cast<const f4*>(&L.ks[st * 32 + 16 + 4 * kb]);
+      const f4 vs0 = *reinterpret_cast<const f4*>(&L.vs[st * 32 + 4 * kb]);
+      const f4 vs1 = *reinterpret_cast<const f4*>(&L.vs[st * 32 + 16 + 4 * kb]);
+      const uint32_t valid = __builtin_amdgcn_readfirstlane(L.valid[st]);
+      const int64_t j0 = (int64_t)p0 + st * 32 - base;
+      const bool whole = valid == ~0u && j0 <= -32;
+      h8 P[R];
+#pragma unroll
+      for (int rt = 0; rt < R; ++rt) {
+        const float qf = L.qf[16 * rt + c];
+        float s[8], v[8];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          s[i] = S[rt][0][i] * ks0[i] * qf, s[4 + i] = S[rt][1][i] * ks1[i] * qf;
+          v[i] = vs0[i], v[4 + i] = vs1[i];
+        }
+        if (!whole) {
+          const int r = row0 + 16 * rt + c, i = r / G;
+          const uint32_t bits = r < nq * G ? valid & seen_bits(a, span.first + i, i, j0) : 0u;
+#pragma unroll
+          for (int e = 0; e < 8; ++e) {
+            const bool on = (bits >> (4 * kb + 16 * (e / 4) + e % 4)) & 1;
+            s[e] = on ? s[e] : -INFINITY;
+            v[e] = on ? v[e] : 0.0f;
+          }
+        }
+        float mx = s[0];
+#pragma unroll
+        for (int e = 1; e < 8; ++e) mx = fmaxf(mx, s[e]);
+        if (__any(mx > m[rt] + 6.0f)) {
+          mx = quad_max(mx);
+          const float mn = mx > m[rt] + 6.0f ? mx : m[rt];
+          const float al = mn == m[rt] ? 1.0f : __builtin_amdgcn_exp2f(m[rt] - mn);
+          m[rt] = mn;
+          l[rt] *= al;
+          sg[rt] *= al;
+          sg[rt] = sg[rt] < kSgMin ? 0.0f : sg[rt];
+          inv[rt] = sg[rt] > 0.0f ? 1.0f / sg[rt] : 0.0f;
+        }
+        const float mu = m[rt] == -INFINITY ? 0.0f : m[rt];
+        float top = 0.0f;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          const float p = __builtin_amdgcn_exp2f(s[e] - mu);
+          l[rt] += p;
+          s[e] = p * v[e];
+          top = fmaxf(top, fabsf(s[e]));
+        }
+        if (__any(top > 256.0f * sg[rt])) {
+          top = quad_max(top);
+          if (top > 256.0f * sg[rt]) {
+            const float ns = fmaxf(top, kSgMin), f = sg[rt] / ns;
+            sg[rt] = ns;
+            inv[rt] = 1.0f / ns;
+#pragma unroll
+            for (int j = 0; j < DB; ++j) O[rt][j] *= f;
+          }
+        }
+#pragma unroll
+        for (int e = 0; e < 8; ++e) P[rt][e] = (_Float16)(s[e] * inv[rt]);
+      }
+
+      // O^T += V^T P^T, one element of d per lane column at a time
+#pragma unroll
+      for (int e = 0; e < 8; ++e)
+#pragma unroll
+        for (int i = 0; i < (VB + 3) / 4; ++i) vr[e].w[i] ^= BITS == 8 ? 0x80808080u : 0x88888888u;
+#pragma unroll
+      for (int j = 0; j < DB; ++j) {
+        union { h2 p[4]; h8 v; } x;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          uint32_t lo = vr[2 * i].w[j * BITS / 32], hi = vr[2 * i + 1].w[j * BITS / 32];
+          if constexpr (BITS == 4) {
+            lo = (lo >> (4 * (j & 1))) & 0x0F0F0F0Fu;
+            hi = (hi >> (4 * (j & 1))) & 0x0F0F0F0Fu;
+          }
+          const uint32_t by = j * BITS / 8 % 4;
+          x.p[i] = to_half<BITS>(__builtin_amdgcn_perm(hi, lo, 0x0c000c00u | (4 + by) << 16 | by));
+        }
+#pragma unroll
+        for (int rt = 0; rt < R; ++rt)
+          O[rt][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(x.v, P[rt], O[rt][j], 0, 0, 0);
+      }
+      if (more) load_v(st + 4);
+    }
+  }
+
+  // ---- the four waves meet, one row tile at a time
+  float* out = reinterpret_cast<float*>(lds_bytes);       // [wave][16][OP]
+  float* ml = out + 4 * 16 * OP;                          // [wave][16][2]
+  const bool direct = pt.used <= 1;
+  const int64_t stride = (int64_t)D + 2;
+#pragma unroll
+  for (int rt = 0; rt < R; ++rt) {
+    __syncthreads();
+    const float ls = quad_sum(l[rt]);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      float* o = out + (wave * 16 + c) * OP + (4 * kb + i) * DB;
+#pragma unroll
+      for (int j = 0; j < DB; ++j) o[j] = O[rt][j][i];
+    }
+    if (kb == 0) ml[(wave * 16 + c) * 2] = m[rt], ml[(wave * 16 + c) * 2 + 1] = ls;
+    // their unit (the codes were taken times 2^-9) in the row's first padding element
+    if (kb == 0) out[(wave * 16 + c) * OP + D] = sg[rt] * 512.0f;
+    __syncthreads();
+    for (int x = tid; x < 16 * (D / 4); x += 256) {
+      const int r = x / (D / 4), d = x % (D / 4) * 4, rr = row0 + 16 * rt + r;
+      if (rr >= nq * G) continue;
+      float M = -INFINITY;
+#pragma unroll
+      for (int w = 0; w < 4; ++w) M = fmaxf(M, ml[(w * 16 + r) * 2]);
+      const float mu = M == -INFINITY ? 0.0f : M;
+      float sum = 0.0f, f[4];
+      f4 o = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+      for (int w = 0; w < 4; ++w) {
+        const float e = __builtin_amdgcn_exp2f(ml[(w * 16 + r) * 2] - mu);
+        sum += ml[(w * 16 + r) * 2 + 1] * e;
+        f[w] = out[(w * 16 + r) * OP + D] * e;
+      }
+      const float by = direct ? (sum == 0.0f ? 0.0f : 1.0f / sum) : 1.0f;
+#pragma unroll
+      for (int w = 0; w < 4; ++w)
+        o += *reinterpret_cast<const f4*>(out + (w * 16 + r) * OP + d) * (f[w] * by);
+      const int64_t t = span.first + rr / G, hq = (int64_t)h * G + rr % G;
+      if (direct) {
+        const int64_t at = t * a.o_ts + hq * a.o_hs + d;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          if (a.type == SONIQ_BF16) static_cast<uint16_t*>(a.out)[at + i] = bf16_bits(o[i]);
+          else static_cast<_Float16*>(a.out)[at + i] = (_Float16)o[i];
+        }
+        if (d == 0 && a.lse)
+          a.lse[t * a.q_heads + hq] = sum == 0.0f ? -INFINITY : (M + __log2f(sum)) * 0.693147181f;
+      } else {
+        float* w = a.work + ((t * a.q_heads + hq) * sp.parts + part) * stride;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) w[2 + d + i] = o[i];
+        if (d == 0) w[0] = M, w[1] = sum;
+      }
+    }
+  }
+}
+
+// One workgroup per (token, query head) joins its sequence's parts: wave w
+// takes parts w, w + 4, ..., then the four meet.
+template <int D>
+__global__ __launch_bounds__(256) void k_kv_join(KvAttend a, KvSplit sp) {
+  constexpr int E = D / 64;
+  __shared__ float out[4][D], ml[4][2];
+  const int hq = blockIdx.y, tid = threadIdx.x, lane = tid % 64, wave = tid / 64;
+  const int64_t t = blockIdx.x;
+  const int b = row_sequence(a.cu, a.table.B, (int)t);
+  if (b >= a.table.B) return;
+  const KvSpan span = kv_span(a.cu[b], a.cu[b + 1], a.T);
+  if (t < span.first || t - span.first >= min(span.count, a.max_q)) return;
+  const KvPart pt = part_of(kv_length(a.table, a.dims, a.kv_len[b]), 0, sp.parts, sp.chunk);
+  if (pt.used <= 1) return;  // written where it was computed
+  const int64_t stride = (int64_t)D + 2;
+  const float* w = a.work + (t * a.q_heads + hq) * sp.parts * stride;
+  float m = -INFINITY, l = 0.0f, o[E] = {};
+  for (int p = wave; p < pt.used; p += 4) {
+    const float* x = w + p * stride;
+    const float pm = x[0], pl = x[1], mn = fmaxf(m, pm);
+    const float mu = mn == -INFINITY ? 0.0f : mn;
+    const float al = __builtin_amdgcn_exp2f(m - mu), be = __builtin_amdgcn_exp2f(pm - mu);
+    l = l * al + pl * be;
+#pragma unroll
+    for (int i = 0; i < E; ++i) o[i] = o[i] * al + x[2 + lane + 64 * i] * be;
+    m = mn;
+  }
+#pragma unroll
+  for (int i = 0; i < E; ++i) out[wave][lane + 64 * i] = o[i];
+  if (lane == 0) ml[wave][0] = m, ml[wave][1] = l;
+  __syncthreads();
+  float M = fmaxf(fmaxf(ml[0][0], ml[1][0]), fmaxf(ml[2][0], ml[3][0]));
+  const float mu = M == -INFINITY ? 0.0f : M;
+  float f[4], sum = 0.0f;
+#pragma unroll
+  for (int x = 0; x < 4; ++x) {
+    f[x] = __builtin_amdgcn_exp2f(ml[x][0] - mu);
+    sum += ml[x][1] * f[x];
+  }
+  const float by = sum == 0.0f ? 0.0f : 1.0f / sum;
+  for (int d = tid; d < D; d += 256) {
+    float y = 0.0f;
+#pragma unroll
+    for (int x = 0; x < 4; ++x) y += out[x][d] * f[x];
+    y *= by;
+    const int64_t at = t * a.o_ts + hq * a.o_hs + d;
+    if (a.type == SONIQ_BF16) static_cast<uint16_t*>(a.out)[at] = bf16_bits(y);
+    else static_cast<_Float16*>(a.out)[at] = (_Float16)y;
+  }
+  if (tid == 0 && a.lse) a.lse[t * a.q_heads + hq] = sum == 0.0f ? -INFINITY : (M + __log2f(sum)) * 0.693147181f;
+}
+
+// Rows a workgroup takes, and how the positions are cut.  At least about a
+// thousand workgroups where the positions give them (two to four a CU are
+// resident), at most about eight thousand, and parts of at most 1024
+// positions a row tile otherwise, so that ragged lengths level out.
+KvSplit kv_split(const KvDims& d, int32_t q_heads, int64_t B, int64_t max_q, int64_t max_kv) {
+  const int64_t rows = max_q * (q_heads / d.heads);
+  KvSplit s;
+  s.R = rows <= 16 ? 1 : rows <= 32 || d.head_dim > 128 ? 2 : 4;
+  s.RB = (int)((rows + 16 * s.R - 1) / (16 * s.R));
+  const int64_t units = B * d.heads * s.RB;
+  auto up = [](int64_t x) { return (x + 127) / 128 * 128; };
+  max_kv = max_kv < 1 ? 1 : max_kv;
+  const int64_t cap = std::max<int64_t>(1024 * s.R, up(max_kv * units / 8192));
+  int64_t chunk = std::min(std::max<int64_t>(up(max_kv * units / 1024), 128), cap);
+  int64_t parts = (max_kv + chunk - 1) / chunk;
+  parts = std::max<int64_t>(1, std::min(parts, (int64_t)(1 << 22) / units));
+  s.chunk = (int)chunk;
+  s.parts = (int)parts;
+  return s;
+}
+
+template <int D, int BITS>
+void launch_attend(const KvAttend& a, const KvSplit& s, hipStream_t stream) {
+  const int64_t u = (int64_t)a.table.B * a.dims.heads * s.parts;
+  const dim3 grid((unsigned)((u + 7) / 8 * 8 * s.RB)), block(256);
+  if (s.R == 1) k_kv_attend<D, BITS, 1><<<grid, block, 0, stream>>>(a, s);
+  else if (s.R == 2) k_kv_attend<D, BITS, 2><<<grid, block, 0, stream>>>(a, s);
+  else if constexpr (D <= 128) k_kv_attend<D, BITS, 4><<<grid, block, 0, stream>>>(a, s);
+  if (s.parts > 1) k_kv_join<D><<<dim3((unsigned)a.T, (unsigned)a.q_heads), 256, 0, stream>>>(a, s);
 }
 
 template <bool WRITE>
@@ -133,12 +629,21 @@ hipError_t launch_kv_copy(const KvCopy& c, hipStream_t stream) {
 hipError_t launch_kv_write(const KvCopy& c, hipStream_t stream) { return launch_kv_copy<true>(c, stream); }
 hipError_t launch_kv_read(const KvCopy& c, hipStream_t stream) { return launch_kv_copy<false>(c, stream); }
 
-int64_t kv_attention_work_bytes(const KvDims&, int64_t, int32_t, int64_t, int64_t, int64_t) { return 0; }
+int64_t kv_attention_work_bytes(const KvDims& d, int64_t T, int32_t q_heads, int64_t B,
+                                int64_t max_q, int64_t max_kv) {
+  const KvSplit s = kv_split(d, q_heads, B, max_q, max_kv);
+  return s.parts > 1 ? T * q_heads * s.parts * (d.head_dim + 2) * 4 : 0;
+}
 
 hipError_t launch_kv_attention(const KvAttend& a, hipStream_t stream) {
-  const dim3 grid((unsigned)a.max_q, (unsigned)a.q_heads, (unsigned)a.table.B), block(256);
-  if (a.type == SONIQ_BF16) k_kv_attend<SONIQ_BF16><<<grid, block, 0, stream>>>(a);
-  else k_kv_attend<SONIQ_F16><<<grid, block, 0, stream>>>(a);
+  const KvSplit s = kv_split(a.dims, a.q_heads, a.table.B, a.max_q, a.max_kv);
+  const bool b8 = a.dims.bits == 8;
+  switch (a.dims.head_dim) {
+    case 64: b8 ? launch_attend<64, 8>(a, s, stream) : launch_attend<64, 4>(a, s, stream); break;
+    case 128: b8 ? launch_attend<128, 8>(a, s, stream) : launch_attend<128, 4>(a, s, stream); break;
+    case 192: b8 ? launch_attend<192, 8>(a, s, stream) : launch_attend<192, 4>(a, s, stream); break;
+    default: b8 ? launch_attend<256, 8>(a, s, stream) : launch_attend<256, 4>(a, s, stream); break;
+  }
   return hipGetLastError();
 }
 
