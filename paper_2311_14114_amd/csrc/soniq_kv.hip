@@ -77,8 +77,11 @@ __global__ __launch_bounds__(64) void k_kv_copy(KvCopy c) {
 // K and V go from memory to registers; LDS holds the queries' fragments and
 // each position's cache row and scales.
 //
-// Codes become fp16 exactly: a code moved to unsigned, u, is read as the
-// fp16 subnormal u * 2^-24, and one packed fma makes it (u - zero) * 2^-9.
+// Codes become fp16 exactly: a code moved to unsigned, u = code + zero, is the
+// fp16 subnormal u * 2^-24.  K goes into the product like that, and the
+// scores start from -zero * 2^-24 * sum(q) (sums of D terms: nothing is
+// lost); V would lose digits over a long context, so one packed fma makes it
+// (u - zero) * 2^-9 first.
 // Queries are scaled by a power of two per row to use fp16's whole range
 // (bf16 queries are exact in it down to 2^-22 of the row's largest element).
 //
@@ -122,8 +125,9 @@ __device__ __forceinline__ float quad_sum(float x) {
   return __uint_as_float(b[0]) + __uint_as_float(b[1]);
 }
 
+// Two V codes moved to unsigned, times 2^-9.
 template <int BITS>
-__device__ __forceinline__ h2 to_half(uint32_t u16pair) {
+__device__ __forceinline__ h2 v_half(uint32_t u16pair) {
   const h2 x = __builtin_bit_cast(h2, u16pair);
   const _Float16 z = BITS == 8 ? (_Float16)-0.25f : (_Float16)-0x1p-6f;
   return __builtin_elementwise_fma(x, h2{(_Float16)32768.0f, (_Float16)32768.0f}, h2{z, z});
@@ -133,18 +137,18 @@ __device__ __forceinline__ h2 to_half(uint32_t u16pair) {
 // from one word of 4-bit codes in the order 0 4 1 5 2 6 3 7.
 template <int BITS>
 __device__ __forceinline__ h8 k_operand(const uint32_t* w) {
-  union { h2 p[4]; h8 v; } r;
+  union { uint32_t p[4]; h8 v; } r;
   if constexpr (BITS == 8) {
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
       const uint32_t u = w[i] ^ 0x80808080u;
-      r.p[2 * i] = to_half<8>(__builtin_amdgcn_perm(u, u, 0x0c010c00u));
-      r.p[2 * i + 1] = to_half<8>(__builtin_amdgcn_perm(u, u, 0x0c030c02u));
+      r.p[2 * i] = __builtin_amdgcn_perm(u, u, 0x0c010c00u);
+      r.p[2 * i + 1] = __builtin_amdgcn_perm(u, u, 0x0c030c02u);
     }
   } else {
     const uint32_t u = w[0] ^ 0x88888888u;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) r.p[i] = to_half<4>((u >> (4 * i)) & 0x000F000Fu);
+    for (int i = 0; i < 4; ++i) r.p[i] = (u >> (4 * i)) & 0x000F000Fu;
   }
   return r.v;
 }
@@ -219,21 +223,22 @@ struct KvPart {
   int first, count, used;  // used: parts of this sequence that hold positions
 };
 __device__ __forceinline__ KvPart part_of(int len, int part, int parts, int chunk) {
-  int64_t c = ((int64_t)len + parts - 1) / parts;
-  c = (c + 127) & ~(int64_t)127;
-  c = c > chunk ? c : chunk;
-  const int64_t first = part * c;
-  const int count = first >= len ? 0 : (int)min(c, len - first);
-  return {(int)first, count, (int)((len + c - 1) / c)};
+  // len < 2^31 and parts <= 2^22, so that nothing here passes 32 bits but the product
+  uint32_t c = ((uint32_t)len + parts - 1) / (uint32_t)parts;
+  c = max((c + 127) & ~127u, (uint32_t)chunk);
+  const uint64_t first = (uint64_t)part * c;
+  const int count = first >= (uint64_t)len ? 0 : (int)min((uint64_t)c, len - first);
+  return {(int)first, count, (int)(((uint32_t)len + c - 1) / c)};
 }
 
 template <int D, int R>
 struct KvLds {
-  int32_t row[kSub];
+  uint32_t row[kSub];
   float ks[kSub], vs[kSub];
   uint32_t valid[kSub / 32];
   h8 q[R][D / 32][64];
-  float qf[16 * R];
+  float qf[16 * R], qz[16 * R];  // per row: unit of the scores, and where they start
+  int32_t qi[16 * R];            // per row: its query, -1 for none
 };
 
 __device__ __forceinline__ float q_value(const void* p, int64_t i, int type) {
@@ -270,7 +275,8 @@ __global__ __launch_bounds__(256, 2) void k_kv_attend(KvAttend a, KvSplit sp) {
   const KvPart pt = part_of(len, part, sp.parts, sp.chunk);
   if (rows <= 0 || (part > 0 && pt.count == 0)) return;
 
-  const int tid = threadIdx.x, lane = tid % 64, wave = tid / 64, c = lane % 16, kb = lane / 16;
+  const int tid = threadIdx.x, lane = tid % 64, c = lane % 16, kb = lane / 16;
+  const int wave = __builtin_amdgcn_readfirstlane(tid / 64);  // uniform, and known to be
 
   // ---- queries: scaled to fp16, in operand order
   {
@@ -297,15 +303,26 @@ __global__ __launch_bounds__(256, 2) void k_kv_attend(KvAttend a, KvSplit sp) {
       // largest element to [2^14, 2^15); rows of zeros, infinities or NaN as they are
       int e = (int)(mx >> 23) - 127 - 14;
       e = mx >= 0x7F800000u || mx == 0 ? 0 : max(e, -100);
-      const float down = __uint_as_float((uint32_t)(127 - e) << 23);
-      if (tid % TPR == 0) L.qf[r] = __uint_as_float((uint32_t)(127 + e) << 23) * 512.0f * (a.scale * 1.44269504f);
+      const float down = copysignf(__uint_as_float((uint32_t)(127 - e) << 23), a.scale);
+      float sum = 0.0f;
 #pragma unroll
       for (int g = 0; g < PER / 8; ++g) {
         h8 v;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) v[k_order<BITS>(i)] = (_Float16)(x[8 * g + i] * down);
+        for (int i = 0; i < 8; ++i) {
+          const _Float16 y = (_Float16)(x[8 * g + i] * down);
+          v[k_order<BITS>(i)] = y;
+          sum += (float)y;
+        }
         const int d = d0 + 8 * g;
         L.q[r / 16][d % (D / 4) / 8][d / (D / 4) * 16 + r % 16] = v;
+      }
+#pragma unroll
+      for (int o = 1; o < TPR; o *= 2) sum += __shfl_xor(sum, o);
+      if (tid % TPR == 0) {
+        L.qf[r] = fabsf(a.scale) * 1.44269504f * 0x1p24f * __uint_as_float((uint32_t)(127 + e) << 23);
+        L.qz[r] = sum * (BITS == 8 ? -0x1p-17f : -0x1p-21f);
+        L.qi[r] = r < rows ? (row0 + r) / G : -1;
       }
     }
   }
@@ -326,16 +343,16 @@ __global__ __launch_bounds__(256, 2) void k_kv_attend(KvAttend a, KvSplit sp) {
   Raw<VB> vr[8];
   auto load_k = [&](int st) {
 #pragma unroll
-    for (int t = 0; t < 2; ++t) kr[t].load(kp + (int64_t)L.row[st * 32 + 16 * t + c] * RB);
+    for (int t = 0; t < 2; ++t) kr[t].load(kp + (uint64_t)L.row[st * 32 + 16 * t + c] * RB);
   };
   auto load_v = [&](int st) {
 #pragma unroll
     for (int t = 0; t < 2; ++t) {
-      const int4 x = *reinterpret_cast<const int4*>(&L.row[st * 32 + 16 * t + 4 * kb]);
-      vr[4 * t].load(vp + (int64_t)x.x * RB);
-      vr[4 * t + 1].load(vp + (int64_t)x.y * RB);
-      vr[4 * t + 2].load(vp + (int64_t)x.z * RB);
-      vr[4 * t + 3].load(vp + (int64_t)x.w * RB);
+      const uint4 x = *reinterpret_cast<const uint4*>(&L.row[st * 32 + 16 * t + 4 * kb]);
+      vr[4 * t].load(vp + (uint64_t)x.x * RB);
+      vr[4 * t + 1].load(vp + (uint64_t)x.y * RB);
+      vr[4 * t + 2].load(vp + (uint64_t)x.z * RB);
+      vr[4 * t + 3].load(vp + (uint64_t)x.w * RB);
     }
   };
 
@@ -371,9 +388,15 @@ __global__ __launch_bounds__(256, 2) void k_kv_attend(KvAttend a, KvSplit sp) {
       const bool more = st + 4 < nst;
       f4 S[R][2];
 #pragma unroll
-      for (int rt = 0; rt < R; ++rt) S[rt][0] = S[rt][1] = f4{0.0f, 0.0f, 0.0f, 0.0f};
+      for (int rt = 0; rt < R; ++rt) {
+        int x = 16 * rt + c;
+        asm volatile("" : "+v"(x));
+        const float z = L.qz[x];
+        S[rt][0] = S[rt][1] = f4{z, z, z, z};
+      }
 #pragma unroll
       for (int s = 0; s < NK; ++s) {
+        if constexpr (D * R > 256) __builtin_amdgcn_sched_barrier(0);
         const h8 k0 = k_operand<BITS>(&kr[0].w[s * (BITS == 8 ? 2 : 1)]);
         const h8 k1 = k_operand<BITS>(&kr[1].w[s * (BITS == 8 ? 2 : 1)]);
 #pragma unroll
@@ -385,29 +408,30 @@ __global__ __launch_bounds__(256, 2) void k_kv_attend(KvAttend a, KvSplit sp) {
       }
       if (more) load_k(st + 4);
 
-      const f4 ks0 = *reinterpret_cast<const f4*>(&L.ks[st * 32 + 4 * kb]);
-      const f4 ks1 = *reinterpret_cast<const f4*>(&L.ks[st * 32 + 16 + 4 * kb]);
-      const f4 vs0 = *reinterpret_cast<const f4*>(&L.vs[st * 32 + 4 * kb]);
-      const f4 vs1 = *reinterpret_cast<const f4*>(&L.vs[st * 32 + 16 + 4 * kb]);
       const uint32_t valid = __builtin_amdgcn_readfirstlane(L.valid[st]);
       const int64_t j0 = (int64_t)p0 + st * 32 - base;
       const bool whole = valid == ~0u && j0 <= -32;
       h8 P[R];
 #pragma unroll
       for (int rt = 0; rt < R; ++rt) {
-        const float qf = L.qf[16 * rt + c];
+        if constexpr (R > 1) __builtin_amdgcn_sched_barrier(0);
+        int x = 16 * rt + c, y = st * 32 + 4 * kb;
+        asm volatile("" : "+v"(x), "+v"(y));  // read here: nothing of this is kept over the row tiles
+        const float qf = L.qf[x];
+        const f4 ks0 = *reinterpret_cast<const f4*>(&L.ks[y]), ks1 = *reinterpret_cast<const f4*>(&L.ks[y + 16]);
+        const f4 vs0 = *reinterpret_cast<const f4*>(&L.vs[y]), vs1 = *reinterpret_cast<const f4*>(&L.vs[y + 16]);
         float s[8], v[8];
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-          s[i] = S[rt][0][i] * ks0[i] * qf, s[4 + i] = S[rt][1][i] * ks1[i] * qf;
+          s[i] = S[rt][0][i] * ks0[i], s[4 + i] = S[rt][1][i] * ks1[i];
           v[i] = vs0[i], v[4 + i] = vs1[i];
         }
         if (!whole) {
-          const int r = row0 + 16 * rt + c, i = r / G;
-          const uint32_t bits = r < nq * G ? valid & seen_bits(a, span.first + i, i, j0) : 0u;
+          const int i = L.qi[x];
+          const uint32_t bits = (i >= 0 ? valid & seen_bits(a, span.first + i, i, j0) : 0u) >> (4 * kb);
 #pragma unroll
           for (int e = 0; e < 8; ++e) {
-            const bool on = (bits >> (4 * kb + 16 * (e / 4) + e % 4)) & 1;
+            const bool on = (bits >> (16 * (e / 4) + e % 4)) & 1;
             s[e] = on ? s[e] : -INFINITY;
             v[e] = on ? v[e] : 0.0f;
           }
@@ -415,6 +439,7 @@ __global__ __launch_bounds__(256, 2) void k_kv_attend(KvAttend a, KvSplit sp) {
         float mx = s[0];
 #pragma unroll
         for (int e = 1; e < 8; ++e) mx = fmaxf(mx, s[e]);
+        mx *= qf;
         if (__any(mx > m[rt] + 6.0f)) {
           mx = quad_max(mx);
           const float mn = mx > m[rt] + 6.0f ? mx : m[rt];
@@ -423,13 +448,13 @@ __global__ __launch_bounds__(256, 2) void k_kv_attend(KvAttend a, KvSplit sp) {
           l[rt] *= al;
           sg[rt] *= al;
           sg[rt] = sg[rt] < kSgMin ? 0.0f : sg[rt];
-          inv[rt] = sg[rt] > 0.0f ? 1.0f / sg[rt] : 0.0f;
+          inv[rt] = sg[rt] > 0.0f ? __builtin_amdgcn_rcpf(sg[rt]) : 0.0f;
         }
         const float mu = m[rt] == -INFINITY ? 0.0f : m[rt];
         float top = 0.0f;
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-          const float p = __builtin_amdgcn_exp2f(s[e] - mu);
+          const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(s[e], qf, -mu));
           l[rt] += p;
           s[e] = p * v[e];
           top = fmaxf(top, fabsf(s[e]));
@@ -437,9 +462,10 @@ __global__ __launch_bounds__(256, 2) void k_kv_attend(KvAttend a, KvSplit sp) {
         if (__any(top > 256.0f * sg[rt])) {
           top = quad_max(top);
           if (top > 256.0f * sg[rt]) {
-            const float ns = fmaxf(top, kSgMin), f = sg[rt] / ns;
+            const float ns = fmaxf(top, kSgMin);
+            inv[rt] = __builtin_amdgcn_rcpf(ns);
+            const float f = sg[rt] * inv[rt];
             sg[rt] = ns;
-            inv[rt] = 1.0f / ns;
 #pragma unroll
             for (int j = 0; j < DB; ++j) O[rt][j] *= f;
           }
@@ -449,12 +475,14 @@ __global__ __launch_bounds__(256, 2) void k_kv_attend(KvAttend a, KvSplit sp) {
       }
 
       // O^T += V^T P^T, one element of d per lane column at a time
+      if constexpr (R > 1) __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
       for (int e = 0; e < 8; ++e)
 #pragma unroll
         for (int i = 0; i < (VB + 3) / 4; ++i) vr[e].w[i] ^= BITS == 8 ? 0x80808080u : 0x88888888u;
 #pragma unroll
       for (int j = 0; j < DB; ++j) {
+        if constexpr (D * R > 256) __builtin_amdgcn_sched_barrier(0);
         union { h2 p[4]; h8 v; } x;
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
@@ -464,7 +492,7 @@ __global__ __launch_bounds__(256, 2) void k_kv_attend(KvAttend a, KvSplit sp) {
             hi = (hi >> (4 * (j & 1))) & 0x0F0F0F0Fu;
           }
           const uint32_t by = j * BITS / 8 % 4;
-          x.p[i] = to_half<BITS>(__builtin_amdgcn_perm(hi, lo, 0x0c000c00u | (4 + by) << 16 | by));
+          x.p[i] = v_half<BITS>(__builtin_amdgcn_perm(hi, lo, 0x0c000c00u | (4 + by) << 16 | by));
         }
 #pragma unroll
         for (int rt = 0; rt < R; ++rt)
@@ -549,15 +577,26 @@ __global__ __launch_bounds__(256) void k_kv_join(KvAttend a, KvSplit sp) {
   const int64_t stride = (int64_t)D + 2;
   const float* w = a.work + (t * a.q_heads + hq) * sp.parts * stride;
   float m = -INFINITY, l = 0.0f, o[E] = {};
-  for (int p = wave; p < pt.used; p += 4) {
-    const float* x = w + p * stride;
-    const float pm = x[0], pl = x[1], mn = fmaxf(m, pm);
-    const float mu = mn == -INFINITY ? 0.0f : mn;
-    const float al = __builtin_amdgcn_exp2f(m - mu), be = __builtin_amdgcn_exp2f(pm - mu);
-    l = l * al + pl * be;
+  // four parts' loads at a time (past the last one: its own again, weightless)
+  for (int p0 = wave; p0 < pt.used; p0 += 16) {
+    float pm[4], pl[4], po[4][E];
 #pragma unroll
-    for (int i = 0; i < E; ++i) o[i] = o[i] * al + x[2 + lane + 64 * i] * be;
-    m = mn;
+    for (int k = 0; k < 4; ++k) {
+      const bool on = p0 + 4 * k < pt.used;
+      const float* x = w + (on ? p0 + 4 * k : p0) * stride;
+      pm[k] = on ? x[0] : -INFINITY, pl[k] = on ? x[1] : 0.0f;
+#pragma unroll
+      for (int i = 0; i < E; ++i) po[k][i] = on ? x[2 + lane + 64 * i] : 0.0f;
+    }
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      const float mn = fmaxf(m, pm[k]), mu = mn == -INFINITY ? 0.0f : mn;
+      const float al = __builtin_amdgcn_exp2f(m - mu), be = __builtin_amdgcn_exp2f(pm[k] - mu);
+      l = l * al + pl[k] * be;  // a part that met a NaN alone has no maximum, but its sum
+#pragma unroll
+      for (int i = 0; i < E; ++i) o[i] = o[i] * al + po[k][i] * be;
+      m = mn;
+    }
   }
 #pragma unroll
   for (int i = 0; i < E; ++i) out[wave][lane + 64 * i] = o[i];
@@ -591,7 +630,7 @@ __global__ __launch_bounds__(256) void k_kv_join(KvAttend a, KvSplit sp) {
 KvSplit kv_split(const KvDims& d, int32_t q_heads, int64_t B, int64_t max_q, int64_t max_kv) {
   const int64_t rows = max_q * (q_heads / d.heads);
   KvSplit s;
-  s.R = rows <= 16 ? 1 : rows <= 32 || d.head_dim > 128 ? 2 : 4;
+  s.R = rows <= 16 ? 1 : rows <= 32 || d.head_dim > 64 ? 2 : 4;
   s.RB = (int)((rows + 16 * s.R - 1) / (16 * s.R));
   const int64_t units = B * d.heads * s.RB;
   auto up = [](int64_t x) { return (x + 127) / 128 * 128; };
@@ -599,7 +638,7 @@ KvSplit kv_split(const KvDims& d, int32_t q_heads, int64_t B, int64_t max_q, int
   const int64_t cap = std::max<int64_t>(1024 * s.R, up(max_kv * units / 8192));
   int64_t chunk = std::min(std::max<int64_t>(up(max_kv * units / 1024), 128), cap);
   int64_t parts = (max_kv + chunk - 1) / chunk;
-  parts = std::max<int64_t>(1, std::min(parts, (int64_t)(1 << 22) / units));
+  parts = std::max<int64_t>(1, std::min(parts, ((int64_t)1 << 22) / units));
   s.chunk = (int)chunk;
   s.parts = (int)parts;
   return s;
@@ -611,7 +650,7 @@ void launch_attend(const KvAttend& a, const KvSplit& s, hipStream_t stream) {
   const dim3 grid((unsigned)((u + 7) / 8 * 8 * s.RB)), block(256);
   if (s.R == 1) k_kv_attend<D, BITS, 1><<<grid, block, 0, stream>>>(a, s);
   else if (s.R == 2) k_kv_attend<D, BITS, 2><<<grid, block, 0, stream>>>(a, s);
-  else if constexpr (D <= 128) k_kv_attend<D, BITS, 4><<<grid, block, 0, stream>>>(a, s);
+  else if constexpr (D <= 64) k_kv_attend<D, BITS, 4><<<grid, block, 0, stream>>>(a, s);
   if (s.parts > 1) k_kv_join<D><<<dim3((unsigned)a.T, (unsigned)a.q_heads), 256, 0, stream>>>(a, s);
 }
 
