@@ -540,7 +540,7 @@ soniq_status soniq_quantize_rows(const void* A_dev, int a_type, int64_t M, int64
  *   bias_dev device, fp32 [N], or NULL
  *   Y_dev    device, y_type [M, ldy]; columns N.. of a row are not written
  * M = 0 is allowed and does nothing.  Errors: INVALID_ARGUMENT, UNSUPPORTED
- * (K > SONIQ_MAX_K, M or N >= 2^31), HIP.
+ * (K > SONIQ_MAX_K, M >= 2^31, N >= 2^26, or M * N / 4096 >= 2^24), HIP.
  */
 soniq_status soniq_i8_gemm(const int8_t* A_dev, int64_t lda, const float* s_a_dev,
                            const int8_t* W_dev, int64_t ldw, const float* s_w_dev,
@@ -590,7 +590,7 @@ soniq_status soniq_quantize_i8_gemm_workspace(int64_t M, int64_t K, int64_t* byt
  * are ignored, and outputs' rows there are left as they were.
  *
  * Supported: head_dim 64, 128, 192, 256; bits 4, 8; pages * heads *
- * page_size < 2^31; table_width * page_size < 2^31.
+ * page_size < 2^31; table_width * page_size < 2^31; B < 2^16; T < 2^24.
  * ---------------------------------------------------------------------- */
 typedef struct {
   void* k_dev;        /* codes, 16-byte aligned */

@@ -1,94 +1,458 @@
 // gfx950 kernels of the 8-bit linear layers with one scale per token and per
 // output channel.
+//
+//   k_rows       codes and scales of rows, one wave or one workgroup a row
+//   k_i8_skinny  few tokens: bound by the weights' bytes; both operands from
+//                memory to registers, the waves of a workgroup split K
+//   k_i8_tile    many tokens: bound by the matrix cores; operands staged
+//                through LDS
 #include "soniq_serve.h"
 #include "soniq_values.h"
+
+#include <algorithm>
 
 namespace soniq {
 namespace {
 
 typedef int v4i __attribute__((ext_vector_type(4)));
+typedef int v16i __attribute__((ext_vector_type(16)));
 
-// One row per workgroup: its largest |x|, then its codes.
-template <int TYPE>
-__global__ __launch_bounds__(256) void k_rows(const typename Value<TYPE>::T* A, int K, int64_t lda,
-                                              int8_t* Q, int64_t ldq, float* s) {
-  __shared__ uint32_t part[4];
-  const int64_t m = blockIdx.x;
-  const typename Value<TYPE>::T* a = A + m * lda;
-  uint32_t mx = 0;
-  for (int k = threadIdx.x; k < K; k += 256)
-    mx = max(mx, __float_as_uint(Value<TYPE>::load(a[k])) & 0x7FFFFFFFu);
-  for (int o = 32; o; o >>= 1) mx = max(mx, (uint32_t)__shfl_xor((int)mx, o));
-  if (threadIdx.x % 64 == 0) part[threadIdx.x / 64] = mx;
-  __syncthreads();
-  mx = max(max(part[0], part[1]), max(part[2], part[3]));
-  const RowCodec rc = row_codec(mx, 127.0f);
-  if (threadIdx.x == 0) s[m] = rc.s;
-  for (int k = threadIdx.x; k < K; k += 256)
-    Q[m * ldq + k] = (int8_t)row_code(rc, Value<TYPE>::load(a[k]));
+// 16 bytes at any address.
+__device__ __forceinline__ v4i load16(const int8_t* p) {
+  struct __attribute__((packed, aligned(1))) P { v4i v; };
+  return reinterpret_cast<const P*>(p)->v;
 }
 
-template <int TYPE>
-__device__ __forceinline__ void store_y(const I8Gemm& g, int64_t m, int64_t n, int acc, float sa,
-                                        float sw) {
-  float y = __fmul_rn(__fmul_rn((float)acc, sa), sw);
-  if (g.bias) y = __fadd_rn(y, g.bias[n]);
-  static_cast<typename Value<TYPE>::T*>(g.Y)[m * g.ldy + n] = Value<TYPE>::store(y);
-}
-
-// 64x64 tile, four waves of 32x32, 64 channels a step through LDS.
-template <int TYPE>
-__global__ __launch_bounds__(256) void k_i8_tile(I8Gemm g) {
-  __shared__ int8_t As[64][80], Bs[64][80];
-  const int64_t m0 = (int64_t)blockIdx.y * 64, n0 = (int64_t)blockIdx.x * 64;
-  const int tid = threadIdx.x, lane = tid % 64, wave = tid / 64;
-  const int wm = (wave & 1) * 32, wn = (wave >> 1) * 32, r = lane % 16, kq = lane / 16;
-  v4i acc[2][2] = {};
-  for (int64_t k0 = 0; k0 < g.K; k0 += 64) {
-    const int row = tid / 4, c = (tid % 4) * 16;
-    for (int e = 0; e < 16; ++e) {
-      const int64_t k = k0 + c + e;
-      As[row][c + e] = m0 + row < g.M && k < g.K ? g.A[(m0 + row) * g.lda + k] : 0;
-      Bs[row][c + e] = n0 + row < g.N && k < g.K ? g.W[(n0 + row) * g.ldw + k] : 0;
-    }
-    __syncthreads();
-    v4i a[2], b[2];
-    for (int i = 0; i < 2; ++i) {
-      a[i] = *reinterpret_cast<const v4i*>(&As[wm + 16 * i + r][16 * kq]);
-      b[i] = *reinterpret_cast<const v4i*>(&Bs[wn + 16 * i + r][16 * kq]);
-    }
-    for (int i = 0; i < 2; ++i)
-      for (int j = 0; j < 2; ++j)
-        acc[i][j] = __builtin_amdgcn_mfma_i32_16x16x64_i8(a[i], b[j], acc[i][j], 0, 0, 0);
-    __syncthreads();
-  }
-  for (int i = 0; i < 2; ++i)
-    for (int j = 0; j < 2; ++j)
-      for (int e = 0; e < 4; ++e) {
-        const int64_t m = m0 + wm + 16 * i + 4 * kq + e, n = n0 + wn + 16 * j + r;
-        if (m < g.M && n < g.N) store_y<TYPE>(g, m, n, acc[i][j][e], g.sa[m], g.sw[n]);
+// Bytes [k, k + 16) of a row of K, zeros from K on; reads nothing outside the row.
+__device__ __forceinline__ v4i load16_to(const int8_t* row, int64_t k, int64_t K) {
+  if (k + 16 <= K) return load16(row + k);
+  v4i r = {0, 0, 0, 0};
+  if (k >= K) return r;
+  if (K >= 16) {  // the row's last 16 bytes, moved down
+    const v4i x = load16(row + K - 16);
+    const int by = (int)(k + 16 - K), w = by / 4, sh = by % 4 * 8;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      uint32_t lo = 0, hi = 0;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        lo = i + w == j ? (uint32_t)x[j] : lo;
+        hi = i + w + 1 == j ? (uint32_t)x[j] : hi;
       }
+      r[i] = (int)(sh ? lo >> sh | hi << (32 - sh) : lo);
+    }
+    return r;
+  }
+  uint32_t b[4] = {0, 0, 0, 0};
+  for (int i = 0; i < 16; ++i)
+    if (k + i < K) b[i / 4] |= (uint32_t)(uint8_t)row[k + i] << (8 * (i % 4));
+  return v4i{(int)b[0], (int)b[1], (int)b[2], (int)b[3]};
+}
+
+__device__ __forceinline__ void lds_barrier() {
+  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup", "local");
+  __builtin_amdgcn_s_barrier();
+  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
+}
+
+// ------------------------------------------------------------ quantizing --
+// Eight elements of a row, as loaded; elements from K on are zeros.
+template <int TYPE>
+struct Eight {
+  typename Value<TYPE>::T v[8];
+  __device__ __forceinline__ void load(const typename Value<TYPE>::T* row, int k, int K) {
+    if (k + 8 <= K) {
+      struct __attribute__((packed, aligned(sizeof(typename Value<TYPE>::T)))) P {
+        typename Value<TYPE>::T v[8];
+      };
+      __builtin_memcpy(v, reinterpret_cast<const P*>(row + k), sizeof v);
+    } else {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) v[i] = k + i < K ? row[k + i] : (typename Value<TYPE>::T)0;
+    }
+  }
+  __device__ __forceinline__ uint32_t amax() const {
+    uint32_t m = 0;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) m = max(m, __float_as_uint(Value<TYPE>::load(v[i])) & 0x7FFFFFFFu);
+    return m;
+  }
+  __device__ __forceinline__ uint2 codes(const RowCoder& c) const {
+    float x[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) x[i] = Value<TYPE>::load(v[i]);
+    int q[8];
+    c.code<8>(x, q);
+    uint32_t w[2];
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+      w[i] = (uint32_t)(q[4 * i] & 255) | (uint32_t)(q[4 * i + 1] & 255) << 8 |
+             (uint32_t)(q[4 * i + 2] & 255) << 16 | (uint32_t)q[4 * i + 3] << 24;
+    return make_uint2(w[0], w[1]);
+  }
+};
+
+__device__ __forceinline__ void store_codes(int8_t* q, int k, int K, uint2 c) {
+  if (k + 8 <= K) {
+    struct __attribute__((packed, aligned(1))) P { uint2 v; };
+    reinterpret_cast<P*>(q + k)->v = c;
+  } else {
+    for (int i = 0; i < 8; ++i)
+      if (k + i < K) q[k + i] = (int8_t)((i < 4 ? c.x : c.y) >> (8 * (i % 4)));
+  }
+}
+
+__device__ __forceinline__ uint32_t wave_max(uint32_t m) {
+#pragma unroll
+  for (int o = 32; o; o >>= 1) m = max(m, (uint32_t)__shfl_xor((int)m, o));
+  return m;
+}
+
+// T threads a row, 256 a workgroup.  A row of up to 8 * T * kHeld elements
+// stays in registers between its maximum and its codes; longer ones are read
+// again for the rest.
+template <int TYPE, int T>
+__global__ __launch_bounds__(256) void k_rows(const typename Value<TYPE>::T* A, int64_t M, int K, int64_t lda,
+                                              int8_t* Q, int64_t ldq, float* s) {
+  constexpr int kHeld = 4;
+  __shared__ uint32_t part[4];
+  const int t = threadIdx.x % T;
+  const int64_t step = (int64_t)gridDim.x * (256 / T);
+  for (int64_t m = (int64_t)blockIdx.x * (256 / T) + threadIdx.x / T; m < M; m += step) {
+    const typename Value<TYPE>::T* a = A + m * lda;
+    Eight<TYPE> x[kHeld];
+#pragma unroll
+    for (int i = 0; i < kHeld; ++i) x[i].load(a, min(8 * (t + T * i), K), K);
+    uint32_t mx = 0;
+#pragma unroll
+    for (int i = 0; i < kHeld; ++i) mx = max(mx, x[i].amax());
+    for (int k = 8 * (t + T * kHeld); k < K; k += 8 * T) {
+      Eight<TYPE> y;
+      y.load(a, k, K);
+      mx = max(mx, y.amax());
+    }
+    mx = wave_max(mx);
+    if constexpr (T == 256) {
+      __syncthreads();  // the last row's maxima have been read
+      if (threadIdx.x % 64 == 0) part[threadIdx.x / 64] = mx;
+      __syncthreads();
+      mx = max(max(part[0], part[1]), max(part[2], part[3]));
+    }
+    const RowCoder rc(mx, 127.0f);
+    if (t == 0) s[m] = rc.s;
+#pragma unroll
+    for (int i = 0; i < kHeld; ++i)
+      if (8 * (t + T * i) < K) store_codes(Q + m * ldq, 8 * (t + T * i), K, x[i].codes(rc));
+    for (int k = 8 * (t + T * kHeld); k < K; k += 8 * T) {
+      Eight<TYPE> y;
+      y.load(a, k, K);
+      store_codes(Q + m * ldq, k, K, y.codes(rc));
+    }
+  }
+}
+
+// --------------------------------------------------------------- outputs --
+__device__ __forceinline__ void store_y(const I8Gemm& g, int64_t at, float y) {
+  if (g.y_type == SONIQ_BF16) static_cast<uint16_t*>(g.Y)[at] = bf16_bits(y);
+  else if (g.y_type == SONIQ_F16) static_cast<_Float16*>(g.Y)[at] = (_Float16)y;
+  else static_cast<float*>(g.Y)[at] = y;
+}
+__device__ __forceinline__ float scaled(int acc, float sa, float sw) {
+  return __fmul_rn(__fmul_rn((float)acc, sa), sw);
+}
+
+// ------------------------------------------------------------ few tokens --
+// A workgroup of eight waves takes 16 * NT output channels and all tokens
+// (at most 16 * MT); wave w takes the 128-byte segments w, w + 8, ... of K.
+// A lane loads 32 bytes of its row per segment, q = lane / 16 choosing which:
+// the two products of a segment then see k in the order
+// 32 q + 16 j + i on both sides, which is as good as any.  Sums meet in LDS.
+template <int MT, int NT>
+__global__ __launch_bounds__(512) void k_i8_skinny(I8Gemm g) {
+  constexpr int U = MT * NT == 1 ? 4 : MT + NT <= 3 ? 3 : 2;  // segments in flight
+  __shared__ int red[8][MT * NT][4][64];
+  const int tid = threadIdx.x, lane = tid % 64, r = lane % 16, q = lane / 16;
+  const int wave = __builtin_amdgcn_readfirstlane(tid / 64);
+  const int64_t n0 = (int64_t)blockIdx.x * (16 * NT);
+  const int8_t *wr[NT], *ar[MT];
+#pragma unroll
+  for (int j = 0; j < NT; ++j) wr[j] = g.W + min(n0 + 16 * j + r, g.N - 1) * g.ldw + 32 * q;
+#pragma unroll
+  for (int i = 0; i < MT; ++i) ar[i] = g.A + min((int64_t)(16 * i + r), g.M - 1) * g.lda + 32 * q;
+  v4i acc[MT][NT] = {};
+  const int full = (int)(g.K / 128);
+  auto mma = [&](const v4i (&w)[NT][2], const v4i (&a)[MT][2]) {
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+#pragma unroll
+      for (int i = 0; i < MT; ++i)
+#pragma unroll
+        for (int j = 0; j < NT; ++j)
+          acc[i][j] = __builtin_amdgcn_mfma_i32_16x16x64_i8(a[i][h], w[j][h], acc[i][j], 0, 0, 0);
+  };
+  int sgm = wave;
+  for (; sgm + 8 * (U - 1) < full; sgm += 8 * U) {
+    v4i w[U][NT][2], a[U][MT][2];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int64_t k = (int64_t)(sgm + 8 * u) * 128;
+#pragma unroll
+      for (int j = 0; j < NT; ++j) w[u][j][0] = load16(wr[j] + k), w[u][j][1] = load16(wr[j] + k + 16);
+#pragma unroll
+      for (int i = 0; i < MT; ++i) a[u][i][0] = load16(ar[i] + k), a[u][i][1] = load16(ar[i] + k + 16);
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u) mma(w[u], a[u]);
+  }
+  for (; sgm < full; sgm += 8) {
+    const int64_t k = (int64_t)sgm * 128;
+    v4i w[NT][2], a[MT][2];
+#pragma unroll
+    for (int j = 0; j < NT; ++j) w[j][0] = load16(wr[j] + k), w[j][1] = load16(wr[j] + k + 16);
+#pragma unroll
+    for (int i = 0; i < MT; ++i) a[i][0] = load16(ar[i] + k), a[i][1] = load16(ar[i] + k + 16);
+    mma(w, a);
+  }
+  if (g.K % 128 && wave == full % 8) {
+    const int64_t k = (int64_t)full * 128 + 32 * q;
+    v4i w[NT][2], a[MT][2];
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+#pragma unroll
+      for (int j = 0; j < NT; ++j) w[j][h] = load16_to(wr[j] - 32 * q, k + 16 * h, g.K);
+#pragma unroll
+      for (int i = 0; i < MT; ++i) a[i][h] = load16_to(ar[i] - 32 * q, k + 16 * h, g.K);
+    }
+    mma(w, a);
+  }
+#pragma unroll
+  for (int i = 0; i < MT; ++i)
+#pragma unroll
+    for (int j = 0; j < NT; ++j)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) red[wave][i * NT + j][e][lane] = acc[i][j][e];
+  __syncthreads();
+  for (int x = tid; x < MT * NT * 256; x += 512) {
+    const int tile = x / 256, e = x / 64 % 4, l = x % 64;
+    const int64_t m = 16 * (tile / NT) + 4 * (l / 16) + e, n = n0 + 16 * (tile % NT) + l % 16;
+    if (m >= g.M || n >= g.N) continue;
+    int sum = 0;
+#pragma unroll
+    for (int w = 0; w < 8; ++w) sum += red[w][tile][e][l];
+    float y = scaled(sum, g.sa[m], g.sw[n]);
+    if (g.bias) y = __fadd_rn(y, g.bias[n]);
+    store_y(g, m * g.ldy + n, y);
+  }
+}
+
+// ----------------------------------------------------------- many tokens --
+// BM x BN tile, four waves of (BM/2) x (BN/2), 128 channels a stage through
+// two LDS buffers.  Rows go from memory to registers one stage ahead and
+// into LDS half a stage ahead, so that any alignment, any bound and the last
+// partial stage are a matter of that load alone.  LDS rows are 128 bytes;
+// the 16-byte chunk c of row r sits at chunk c ^ (r / 2 % 8), which spreads
+// the 16 rows that a fragment read touches at once over all banks.  Within a
+// stage the fragments of the next 32 channels are read before the products
+// of these, across the barrier too.
+// Off: type of a row's offset in its tile (64 bits for row strides of 2^24
+// bytes and more).
+template <int BM, int BN, class Off>
+__global__ __launch_bounds__(256, BM * BN > 128 * 128 ? 1 : 2) void k_i8_tile(I8Gemm g, int tm, int tn) {
+  constexpr int TM = BM / 64, TN = BN / 64;        // 32x32 tiles a wave
+  constexpr int LA = BM / 32, LB = BN / 32;        // 16-byte loads a thread and stage
+  __shared__ __align__(16) int8_t lds[2][(BM + BN) * 128];
+
+  // Workgroup b runs on XCD b % 8: each XCD takes a contiguous run of the
+  // tile order, columns of four row blocks, so that its L2 serves the rows
+  // that its tiles share.
+  int bm, bn;
+  {
+    const int total = tm * tn, per = (total + 7) / 8;
+    const int t = (int)(blockIdx.x % 8) * per + (int)(blockIdx.x / 8);
+    if ((int)(blockIdx.x / 8) >= per || t >= total) return;
+    const int band = t / (4 * tn), rows = min(4, tm - 4 * band), in = t - band * 4 * tn;
+    bm = 4 * band + in % rows;
+    bn = in / rows;
+  }
+  const int tid = threadIdx.x, lane = tid % 64;
+  const int wave = __builtin_amdgcn_readfirstlane(tid / 64);
+  const int64_t m0 = (int64_t)bm * BM, n0 = (int64_t)bn * BN;
+  const int lr = tid / 8, lc = tid % 8;
+  const int8_t *ta = g.A + m0 * g.lda, *tb = g.W + n0 * g.ldw;
+  Off oa[LA], ob[LB];
+#pragma unroll
+  for (int i = 0; i < LA; ++i) oa[i] = (Off)(min((int64_t)(lr + 32 * i), g.M - 1 - m0) * g.lda) + 16 * lc;
+#pragma unroll
+  for (int i = 0; i < LB; ++i) ob[i] = (Off)(min((int64_t)(lr + 32 * i), g.N - 1 - n0) * g.ldw) + 16 * lc;
+  v4i ra[LA], rb[LB];
+  const int stages = (int)((g.K + 127) / 128);
+  const bool tail = g.K % 128 != 0;
+  // In a partial last stage, chunks that cross the end of a row are taken from
+  // its last 16 bytes (K >= 16 here) and moved down when they are written;
+  // `over`: how many bytes past the end this thread's chunk would reach.
+  const int over = max(0, 16 * lc + 16 - (int)(g.K - (int64_t)(stages - 1) * 128));
+  auto load = [&](int s) {
+    const int64_t k = (int64_t)s * 128 - 128;
+    const int at = 128 - (s == stages - 1 ? over : 0);  // 1 .. 128
+#pragma unroll
+    for (int i = 0; i < LA; ++i) ra[i] = load16(ta + k + (oa[i] + at));
+#pragma unroll
+    for (int i = 0; i < LB; ++i) rb[i] = load16(tb + k + (ob[i] + at));
+  };
+  auto move_down = [&](v4i& x) {
+    const uint64_t lo = (uint32_t)x[0] | (uint64_t)(uint32_t)x[1] << 32;
+    const uint64_t hi = (uint32_t)x[2] | (uint64_t)(uint32_t)x[3] << 32;
+    const int sh = 8 * (over & 7);
+    const uint64_t up = sh ? hi << (64 - sh) : 0, l = over & 8 ? hi >> sh : lo >> sh | up;
+    const uint64_t h = over & 8 ? 0 : hi >> sh;
+    x[0] = over >= 16 ? 0 : (int)l, x[1] = over >= 16 ? 0 : (int)(l >> 32);
+    x[2] = over >= 16 ? 0 : (int)h, x[3] = over >= 16 ? 0 : (int)(h >> 32);
+  };
+  const int wat = lr * 128 + ((lc ^ (lr / 2 % 8)) << 4);
+  auto write = [&](int buf, int s) {
+    if (tail && s == stages - 1) {
+      asm volatile("");  // a branch, not selects in every stage
+#pragma unroll
+      for (int i = 0; i < LA; ++i) move_down(ra[i]);
+#pragma unroll
+      for (int i = 0; i < LB; ++i) move_down(rb[i]);
+    }
+#pragma unroll
+    for (int i = 0; i < LA; ++i) *reinterpret_cast<v4i*>(&lds[buf][wat + 4096 * i]) = ra[i];
+#pragma unroll
+    for (int i = 0; i < LB; ++i) *reinterpret_cast<v4i*>(&lds[buf][BM * 128 + wat + 4096 * i]) = rb[i];
+  };
+  const int wm = (wave & 1) * (BM / 2), wn = (wave >> 1) * (BN / 2);
+  int rat[4];
+#pragma unroll
+  for (int ks = 0; ks < 4; ++ks)
+    rat[ks] = (lane % 32) * 128 + (((2 * ks + lane / 32) ^ (lane / 2 % 8)) << 4);
+  struct Frag {
+    v4i a[TM], b[TN];
+  } f[2];
+  auto read = [&](Frag& x, int buf, int ks) {
+#pragma unroll
+    for (int i = 0; i < TM; ++i) x.a[i] = *reinterpret_cast<const v4i*>(&lds[buf][rat[ks] + (wm + 32 * i) * 128]);
+#pragma unroll
+    for (int j = 0; j < TN; ++j)
+      x.b[j] = *reinterpret_cast<const v4i*>(&lds[buf][rat[ks] + (BM + wn + 32 * j) * 128]);
+  };
+  v16i acc[TM][TN];
+#pragma unroll
+  for (int i = 0; i < TM; ++i)
+#pragma unroll
+    for (int j = 0; j < TN; ++j)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) acc[i][j][e] = 0;
+  auto mma = [&](const Frag& x) {
+#pragma unroll
+    for (int i = 0; i < TM; ++i)
+#pragma unroll
+      for (int j = 0; j < TN; ++j)
+        acc[i][j] = __builtin_amdgcn_mfma_i32_32x32x32_i8(x.a[i], x.b[j], acc[i][j], 0, 0, 0);
+  };
+
+  load(0);
+  write(0, 0);
+  if (stages > 1) load(1);
+  lds_barrier();
+  read(f[0], 0, 0);
+  for (int s = 0; s < stages; ++s) {
+    const int buf = s & 1;
+    read(f[1], buf, 1);
+    mma(f[0]);
+    __builtin_amdgcn_sched_barrier(0);
+    read(f[0], buf, 2);
+    mma(f[1]);
+    __builtin_amdgcn_sched_barrier(0);
+    read(f[1], buf, 3);
+    if (s + 1 < stages) write(buf ^ 1, s + 1);
+    if (s + 2 < stages) load(s + 2);
+    mma(f[0]);
+    __builtin_amdgcn_sched_barrier(0);
+    lds_barrier();
+    if (s + 1 < stages) read(f[0], buf ^ 1, 0);
+    mma(f[1]);
+    __builtin_amdgcn_sched_barrier(0);
+  }
+
+#pragma unroll
+  for (int j = 0; j < TN; ++j) {
+    const int64_t n = n0 + wn + 32 * j + lane % 32;
+    const float sw = n < g.N ? g.sw[n] : 0.0f, bias = g.bias && n < g.N ? g.bias[n] : 0.0f;
+#pragma unroll
+    for (int i = 0; i < TM; ++i)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) {
+        const int64_t m = m0 + wm + 32 * i + 8 * (e / 4) + 4 * (lane / 32) + e % 4;
+        if (m >= g.M || n >= g.N) continue;
+        float y = scaled(acc[i][j][e], g.sa[m], sw);
+        if (g.bias) y = __fadd_rn(y, bias);
+        store_y(g, m * g.ldy + n, y);
+      }
+  }
+}
+
+// Many tokens of fewer than 16 channels: one output a thread.
+__global__ __launch_bounds__(256) void k_i8_short(I8Gemm g) {
+  const int64_t n = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  if (n >= g.N) return;
+  for (int64_t m = blockIdx.y; m < g.M; m += gridDim.y) {
+    int sum = 0;
+    for (int k = 0; k < g.K; ++k) sum += (int)g.A[m * g.lda + k] * (int)g.W[n * g.ldw + k];
+    float y = scaled(sum, g.sa[m], g.sw[n]);
+    if (g.bias) y = __fadd_rn(y, g.bias[n]);
+    store_y(g, m * g.ldy + n, y);
+  }
+}
+
+template <int TYPE>
+void launch_rows(const void* A, int64_t M, int64_t K, int64_t lda, int8_t* Q, int64_t ldq, float* s,
+                 hipStream_t stream) {
+  const auto* a = static_cast<const typename Value<TYPE>::T*>(A);
+  if (K <= 2048 && M > 256) {
+    const unsigned grid = (unsigned)std::min<int64_t>((M + 3) / 4, 1 << 20);
+    k_rows<TYPE, 64><<<grid, 256, 0, stream>>>(a, M, (int)K, lda, Q, ldq, s);
+  } else {
+    const unsigned grid = (unsigned)std::min<int64_t>(M, 1 << 20);
+    k_rows<TYPE, 256><<<grid, 256, 0, stream>>>(a, M, (int)K, lda, Q, ldq, s);
+  }
+}
+
+template <int BM, int BN, class Off>
+void launch_tile(const I8Gemm& g, hipStream_t stream) {
+  const int64_t tm = (g.M + BM - 1) / BM, tn = (g.N + BN - 1) / BN;
+  k_i8_tile<BM, BN, Off><<<(unsigned)((tm * tn + 7) / 8 * 8), 256, 0, stream>>>(g, (int)tm, (int)tn);
+}
+
+template <int MT>
+void launch_skinny(const I8Gemm& g, hipStream_t stream) {
+  if (MT <= 2 || g.N <= 4096)
+    k_i8_skinny<MT, 1><<<(unsigned)((g.N + 15) / 16), 512, 0, stream>>>(g);
+  else
+    k_i8_skinny<MT, 2><<<(unsigned)((g.N + 31) / 32), 512, 0, stream>>>(g);
 }
 
 }  // namespace
 
 hipError_t launch_quantize_rows(const void* A, int a_type, int64_t M, int64_t K, int64_t lda,
                                 int8_t* Q, int64_t ldq, float* s, hipStream_t stream) {
-  const dim3 grid((unsigned)M), block(256);
-  if (a_type == SONIQ_F32)
-    k_rows<SONIQ_F32><<<grid, block, 0, stream>>>(static_cast<const float*>(A), (int)K, lda, Q, ldq, s);
-  else if (a_type == SONIQ_BF16)
-    k_rows<SONIQ_BF16><<<grid, block, 0, stream>>>(static_cast<const uint16_t*>(A), (int)K, lda, Q, ldq, s);
-  else
-    k_rows<SONIQ_F16><<<grid, block, 0, stream>>>(static_cast<const _Float16*>(A), (int)K, lda, Q, ldq, s);
+  if (a_type == SONIQ_F32) launch_rows<SONIQ_F32>(A, M, K, lda, Q, ldq, s, stream);
+  else if (a_type == SONIQ_BF16) launch_rows<SONIQ_BF16>(A, M, K, lda, Q, ldq, s, stream);
+  else launch_rows<SONIQ_F16>(A, M, K, lda, Q, ldq, s, stream);
   return hipGetLastError();
 }
 
 hipError_t launch_i8_gemm(const I8Gemm& g, hipStream_t stream) {
-  const dim3 grid((unsigned)((g.N + 63) / 64), (unsigned)((g.M + 63) / 64)), block(256);
-  if (g.y_type == SONIQ_F32) k_i8_tile<SONIQ_F32><<<grid, block, 0, stream>>>(g);
-  else if (g.y_type == SONIQ_BF16) k_i8_tile<SONIQ_BF16><<<grid, block, 0, stream>>>(g);
-  else k_i8_tile<SONIQ_F16><<<grid, block, 0, stream>>>(g);
+  if (g.M <= 16) launch_skinny<1>(g, stream);
+  else if (g.M <= 32) launch_skinny<2>(g, stream);
+  else if (g.M <= 48) launch_skinny<3>(g, stream);
+  else if (g.M <= 64) launch_skinny<4>(g, stream);
+  else if (g.K < 16) k_i8_short<<<dim3((unsigned)((g.N + 255) / 256), (unsigned)std::min<int64_t>(g.M, 65535)), 256, 0, stream>>>(g);
+  else if (std::max(g.lda, g.ldw) >= 1 << 24) launch_tile<64, 64, uint64_t>(g, stream);
+  else if (((g.M + 255) / 256) * ((g.N + 255) / 256) >= 200) launch_tile<256, 256, uint32_t>(g, stream);
+  else if (((g.M + 127) / 128) * ((g.N + 127) / 128) >= 200) launch_tile<128, 128, uint32_t>(g, stream);
+  else launch_tile<64, 64, uint32_t>(g, stream);
   return hipGetLastError();
 }
 

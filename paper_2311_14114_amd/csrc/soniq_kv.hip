@@ -16,46 +16,81 @@ __device__ __forceinline__ int row_sequence(const int32_t* cu, int B, int t) {
   return b;
 }
 
-__device__ __forceinline__ int code_at(const uint8_t* row, int d, int bits) {
-  if (bits == 8) return (int8_t)row[d];
-  const int n = (row[d / 2] >> (4 * (d & 1))) & 15;
-  return n - 16 * (n > 7);
-}
+// A row of D elements is D / 8 lanes' work, 16 lanes for 64 elements too (8
+// of them idle), so that every row starts at a lane that 16 divides.  A wave
+// takes 64 / L rows: those of one token, heads of both sides in order.
+template <int D>
+constexpr int kRowLanes = D <= 128 ? 16 : 32;
 
-// One wave per (token, side, head).
-template <int TYPE, bool WRITE>
-__global__ __launch_bounds__(64) void k_kv_copy(KvCopy c) {
+template <int TYPE, int D, int BITS, bool WRITE>
+__global__ __launch_bounds__(256) void k_kv_copy(KvCopy c) {
   typedef typename Value<TYPE>::T T;
-  const int t = blockIdx.x, h = blockIdx.y, lane = threadIdx.x, D = c.dims.head_dim;
-  const KvSide sd = blockIdx.z ? c.side[1] : c.side[0];
+  constexpr int L = kRowLanes<D>, PER = 64 / L, CB = BITS;  // CB: bytes of 8 codes
+  const int lane = threadIdx.x % 64, sub = lane / L, d = lane % L * 8;
+  const int H = c.dims.heads;
+  const int t = (int)blockIdx.x;
+  const int y = ((int)blockIdx.y * 4 + (int)threadIdx.x / 64) * PER + sub;  // row of the token
+  if (y - sub >= 2 * H) return;
+  const bool row_on = y < 2 * H, on = row_on && d < D;
+  const int h = y >= H ? y - H : y;
+  const bool second = y >= H;
+  const int64_t at = second ? (int64_t)t * c.side[1].token_stride + (int64_t)h * c.side[1].head_stride
+                            : (int64_t)t * c.side[0].token_stride + (int64_t)h * c.side[0].head_stride;
+  T* x = static_cast<T*>(second ? c.side[1].rows : c.side[0].rows) + at + d;
+  struct __attribute__((packed, aligned(sizeof(T)))) P { T v[8]; };
+  P v;
+  if (WRITE && on) v = *reinterpret_cast<const P*>(x);
+
   const int b = row_sequence(c.cu, c.table.B, t);
   if (b >= c.table.B) return;
-  const int64_t pos = (int64_t)c.start[b] + ((int64_t)t - c.cu[b]);
-  const int32_t row0 = kv_row(c.table, c.dims, b, pos);
-  T* x = static_cast<T*>(sd.rows) + (int64_t)t * sd.token_stride + h * sd.head_stride;
-  if (row0 < 0) {
-    if (!WRITE)
-      for (int d = lane; d < D; d += 64) x[d] = Value<TYPE>::store(0.0f);
-    return;
-  }
+  const int32_t row0 = kv_row(c.table, c.dims, b, (int64_t)c.start[b] + ((int64_t)t - c.cu[b]));
   const int64_t row = (int64_t)row0 + (int64_t)h * c.dims.page_size;
-  uint8_t* codes = sd.codes + row * (D * c.dims.bits / 8);
+  uint8_t* codes = (second ? c.side[1].codes : c.side[0].codes) + row * (D * BITS / 8) + d * BITS / 8;
+  float* scale = (second ? c.side[1].scale : c.side[0].scale) + row;
   if (WRITE) {
+    if (row0 < 0) return;
+    float f[8];
     uint32_t mx = 0;
-    for (int d = lane; d < D; d += 64) mx = max(mx, __float_as_uint(Value<TYPE>::load(x[d])) & 0x7FFFFFFFu);
-    for (int o = 32; o; o >>= 1) mx = max(mx, (uint32_t)__shfl_xor((int)mx, o));
-    const RowCodec rc = row_codec(mx, c.dims.bits == 8 ? 127.0f : 7.0f);
-    if (lane == 0) sd.scale[row] = rc.s;
-    if (c.dims.bits == 8) {
-      for (int d = lane; d < D; d += 64) codes[d] = (uint8_t)row_code(rc, Value<TYPE>::load(x[d]));
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      f[i] = on ? Value<TYPE>::load(v.v[i]) : 0.0f;
+      mx = max(mx, __float_as_uint(f[i]) & 0x7FFFFFFFu);
+    }
+#pragma unroll
+    for (int o = 1; o < L; o *= 2) mx = max(mx, (uint32_t)__shfl_xor((int)mx, o));
+    const RowCoder rc(mx, BITS == 8 ? 127.0f : 7.0f);
+    if (row_on && d == 0) *scale = rc.s;
+    int q[8];
+    rc.code<8>(f, q);
+    if (!on) return;
+    if constexpr (BITS == 8) {
+      uint32_t w[2];
+#pragma unroll
+      for (int i = 0; i < 2; ++i)
+        w[i] = (uint32_t)(q[4 * i] & 255) | (uint32_t)(q[4 * i + 1] & 255) << 8 |
+               (uint32_t)(q[4 * i + 2] & 255) << 16 | (uint32_t)q[4 * i + 3] << 24;
+      *reinterpret_cast<uint2*>(codes) = make_uint2(w[0], w[1]);
     } else {
-      for (int d = lane; d < D / 2; d += 64)
-        codes[d] = (uint8_t)((row_code(rc, Value<TYPE>::load(x[2 * d])) & 15) |
-                             (row_code(rc, Value<TYPE>::load(x[2 * d + 1])) << 4));
+      uint32_t w = 0;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) w |= (uint32_t)(q[i] & 15) << (4 * i);
+      *reinterpret_cast<uint32_t*>(codes) = w;
     }
   } else {
-    const float s = sd.scale[row];
-    for (int d = lane; d < D; d += 64) x[d] = Value<TYPE>::store((float)code_at(codes, d, c.dims.bits) * s);
+    if (!on) return;
+    uint32_t w[2] = {0, 0};
+    float s = 0.0f;
+    if (row0 >= 0) {
+      s = *scale;
+      w[0] = *reinterpret_cast<const uint32_t*>(codes);
+      if (BITS == 8) w[1] = *reinterpret_cast<const uint32_t*>(codes + 4);
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const int code = BITS == 8 ? (int8_t)(w[i / 4] >> (8 * (i % 4))) : (int)(w[0] << (28 - 4 * i)) >> 28;
+      v.v[i] = Value<TYPE>::store((float)code * s);
+    }
+    *reinterpret_cast<P*>(x) = v;
   }
 }
 
@@ -654,12 +689,23 @@ void launch_attend(const KvAttend& a, const KvSplit& s, hipStream_t stream) {
   if (s.parts > 1) k_kv_join<D><<<dim3((unsigned)a.T, (unsigned)a.q_heads), 256, 0, stream>>>(a, s);
 }
 
+template <bool WRITE, int D, int BITS>
+void launch_kv_copy(const KvCopy& c, hipStream_t stream) {
+  constexpr int PER = 64 / kRowLanes<D>;
+  const dim3 grid((unsigned)c.T, (unsigned)((2 * c.dims.heads + 4 * PER - 1) / (4 * PER)));
+  if (c.type == SONIQ_F32) k_kv_copy<SONIQ_F32, D, BITS, WRITE><<<grid, 256, 0, stream>>>(c);
+  else if (c.type == SONIQ_BF16) k_kv_copy<SONIQ_BF16, D, BITS, WRITE><<<grid, 256, 0, stream>>>(c);
+  else k_kv_copy<SONIQ_F16, D, BITS, WRITE><<<grid, 256, 0, stream>>>(c);
+}
 template <bool WRITE>
 hipError_t launch_kv_copy(const KvCopy& c, hipStream_t stream) {
-  const dim3 grid((unsigned)c.T, (unsigned)c.dims.heads, 2), block(64);
-  if (c.type == SONIQ_F32) k_kv_copy<SONIQ_F32, WRITE><<<grid, block, 0, stream>>>(c);
-  else if (c.type == SONIQ_BF16) k_kv_copy<SONIQ_BF16, WRITE><<<grid, block, 0, stream>>>(c);
-  else k_kv_copy<SONIQ_F16, WRITE><<<grid, block, 0, stream>>>(c);
+  const bool b8 = c.dims.bits == 8;
+  switch (c.dims.head_dim) {
+    case 64: b8 ? launch_kv_copy<WRITE, 64, 8>(c, stream) : launch_kv_copy<WRITE, 64, 4>(c, stream); break;
+    case 128: b8 ? launch_kv_copy<WRITE, 128, 8>(c, stream) : launch_kv_copy<WRITE, 128, 4>(c, stream); break;
+    case 192: b8 ? launch_kv_copy<WRITE, 192, 8>(c, stream) : launch_kv_copy<WRITE, 192, 4>(c, stream); break;
+    default: b8 ? launch_kv_copy<WRITE, 256, 8>(c, stream) : launch_kv_copy<WRITE, 256, 4>(c, stream); break;
+  }
   return hipGetLastError();
 }
 

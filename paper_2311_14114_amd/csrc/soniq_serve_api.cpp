@@ -38,6 +38,7 @@ soniq_status fail(soniq_status st, const char* fmt, ...) {
   } while (0)
 
 constexpr int64_t kMax31 = (int64_t)1 << 31;
+constexpr int64_t kMaxGroups = (int64_t)1 << 24;  // workgroups of 256 threads in a launch
 
 int type_size(int type) { return type == SONIQ_F32 ? 4 : type == SONIQ_BF16 || type == SONIQ_F16 ? 2 : 0; }
 
@@ -70,9 +71,9 @@ soniq_status check_gemm(const char* who, const void* W, int64_t ldw, const float
   NEED(W && s_w && (Y || M == 0), "%s: null pointer", who);
   NEED(aligned(s_w, 4) && aligned(bias, 4) && aligned(Y, type_size(y_type)),
        "%s: s_w, bias or Y is not aligned to its elements", who);
-  LIMIT(K <= SONIQ_MAX_K && M < kMax31 && N < kMax31,
-        "%s: M = %lld, N = %lld, K = %lld (M, N < 2^31, K <= %d)", who, (long long)M, (long long)N,
-        (long long)K, SONIQ_MAX_K);
+  LIMIT(K <= SONIQ_MAX_K && M < kMax31 && N < kMax31 / 32 && ((M + 63) / 64) * ((N + 63) / 64) < kMaxGroups,
+        "%s: M = %lld, N = %lld, K = %lld (M < 2^31, N < 2^26, M * N / 4096 < 2^24, K <= %d)", who,
+        (long long)M, (long long)N, (long long)K, SONIQ_MAX_K);
   return SONIQ_OK;
 }
 
@@ -109,8 +110,8 @@ soniq_status check_table(const char* who, const soniq_kv_cache_t* c, const int32
        (long long)width, (long long)ld);
   NEED((table && cu && other) || B == 0 || T == 0, "%s: null table, cu or lengths", who);
   NEED(aligned(table, 4) && aligned(cu, 4) && aligned(other, 4), "%s: tables are int32, 4-byte aligned", who);
-  LIMIT(B <= 65535 && T < kMax31 && width < kMax31 && width * (int64_t)c->page_size < kMax31,
-        "%s: B = %lld, T = %lld, table_width = %lld (B < 2^16, T and table_width * page_size < 2^31)",
+  LIMIT(B <= 65535 && T < kMaxGroups && width < kMax31 && width * (int64_t)c->page_size < kMax31,
+        "%s: B = %lld, T = %lld, table_width = %lld (B < 2^16, T < 2^24, table_width * page_size < 2^31)",
         who, (long long)B, (long long)T, (long long)width);
   return SONIQ_OK;
 }
@@ -144,9 +145,12 @@ soniq_status check_attend(const char* who, const soniq_kv_cache_t* cache, int64_
        q_heads, cache->heads);
   NEED(T >= 0 && B >= 0 && max_q >= 1 && max_kv >= 0, "%s: T = %lld, B = %lld, max_q = %lld, max_kv = %lld",
        who, (long long)T, (long long)B, (long long)max_q, (long long)max_kv);
-  LIMIT(max_q <= 256 && q_heads <= 65535 && B <= 65535 && max_kv < kMax31 && T * q_heads < kMax31,
-        "%s: max_q = %lld, %d query heads, B = %lld, T = %lld (max_q <= 256, heads and B < 2^16, T * heads < 2^31)",
+  LIMIT(max_q <= 256 && q_heads <= 65535 && B <= 65535 && max_kv < kMax31 && T < kMaxGroups,
+        "%s: max_q = %lld, %d query heads, B = %lld, T = %lld (max_q <= 256, heads and B < 2^16, T < 2^24)",
         who, (long long)max_q, q_heads, (long long)B, (long long)T);
+  LIMIT(B * cache->heads * ((max_q * (q_heads / cache->heads) + 15) / 16) < (1 << 22),
+        "%s: %lld sequences of %d heads and up to %lld new tokens are too many", who, (long long)B,
+        cache->heads, (long long)max_q);
   return SONIQ_OK;
 }
 

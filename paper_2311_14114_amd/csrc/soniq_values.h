@@ -39,32 +39,42 @@ struct Value<SONIQ_F16> {
   static __device__ __forceinline__ T store(float x) { return (_Float16)x; }
 };
 
-// N elements at any element-aligned address, in the widest loads and stores
-// there are (the hardware takes them at any alignment).
-template <class T, int N>
-struct alignas(1) Pack {
-  T v[N];
-} __attribute__((packed));
-
 // The symmetric codec of a row whose largest |x| has the bits `amax` (as an
-// unsigned integer, so that a NaN or an infinity is the largest): its scale,
-// and its codes' range.  A scale of 0, infinity or NaN gives codes 0.
-struct RowCodec {
-  float s;
-  bool zero;
-  float top;
+// unsigned integer, so that a NaN or an infinity is the largest):
+// s = amax / top, code = rint(x / s), both divisions IEEE fp32.  A scale of 0,
+// infinity or NaN gives codes 0.
+//
+// The quotient comes from a reciprocal: v_rcp_f32 is good to one ulp, so for
+// |x / s| <= 128 the product is off by less than 2^-15, and rint of it is
+// rint of the true quotient's fp32 rounding unless it lies within 2^-14 of a
+// half-integer.  There, and for scales near the ends of fp32, the division
+// decides.  The clamp is for subnormal scales, whose own rounding can exceed
+// a step.
+struct RowCoder {
+  float s, rs, top;
+  bool zero, fast;
+  __device__ __forceinline__ RowCoder(uint32_t amax, float top_) : top(top_) {
+    s = __fdiv_rn(__uint_as_float(amax), top);
+    zero = !(s > 0.0f) || amax >= 0x7F800000u;
+    fast = s >= 0x1p-100f && s <= 0x1p100f;
+    rs = __builtin_amdgcn_rcpf(s);
+  }
+  template <int N>
+  __device__ __forceinline__ void code(const float (&x)[N], int (&q)[N]) const {
+    float t[N], far = 0.0f;
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      const float e = x[i] * rs;
+      t[i] = __builtin_rintf(e);
+      far = fmaxf(far, fabsf(e - t[i]));  // at most a half
+    }
+    if (!fast || far >= 0.5f - 0x1p-14f) {
+#pragma unroll
+      for (int i = 0; i < N; ++i) t[i] = fminf(fmaxf(__builtin_rintf(__fdiv_rn(x[i], s)), -top), top);
+    }
+#pragma unroll
+    for (int i = 0; i < N; ++i) q[i] = zero ? 0 : (int)t[i];
+  }
 };
-__device__ __forceinline__ RowCodec row_codec(uint32_t amax, float top) {
-  RowCodec r;
-  r.s = __fdiv_rn(__uint_as_float(amax), top);
-  r.zero = !(r.s > 0.0f) || amax >= 0x7F800000u;
-  r.top = top;
-  return r;
-}
-__device__ __forceinline__ int row_code(const RowCodec& r, float x) {
-  if (r.zero) return 0;
-  // the clamp is for subnormal scales, whose own rounding can exceed a step
-  return (int)fminf(fmaxf(__builtin_rintf(__fdiv_rn(x, r.s)), -r.top), r.top);
-}
 
 }  // namespace soniq
