@@ -10,6 +10,7 @@ every step runs in the library's HIP kernels.  There is no CPU fallback: if
 from __future__ import annotations
 
 import ctypes
+import functools
 import os
 
 import numpy as np
@@ -505,48 +506,86 @@ def soniq_act_wait_timeouts(act: Activations) -> int:
 
 
 # ---- 8-bit linear layers, and the quantized key/value cache -----------------
+# These calls take a few microseconds of GPU time at decode sizes, so their
+# checks are written to cost little: one query of the device and the stream a
+# call, sizes of workspaces remembered by their arguments.
 _TYPES = None
 
 
 def _types():
     global _TYPES
-    if _TYPES is None:
-        import torch
-        _TYPES = {torch.float32: SONIQ_F32, torch.bfloat16: SONIQ_BF16, torch.float16: SONIQ_F16}
+    import torch
+    _TYPES = {torch.float32: SONIQ_F32, torch.bfloat16: SONIQ_BF16, torch.float16: SONIQ_F16,
+              torch.int8: None, torch.int32: None, torch.uint8: None, torch.int64: None}
     return _TYPES
 
 
-def _here(t, what: str, dtype=None, dim=None):
-    """Checks that t is a tensor on the current device (of that type and number
-    of dimensions); the library works on the current device alone."""
+def _device(t, what: str) -> int:
+    """Index of the current device, where t has to be: the library works on the
+    current device alone."""
     import torch
     if not isinstance(t, torch.Tensor) or not t.is_cuda:
         raise TypeError(f"{what} must be a device tensor")
-    if t.device.index != torch.cuda.current_device():
-        raise ValueError(f"{what} is on {t.device}, the current device is cuda:{torch.cuda.current_device()}")
-    if dtype is not None and t.dtype is not dtype:
+    d = torch._C._cuda_getDevice()
+    if t.get_device() != d:
+        raise ValueError(f"{what} is on {t.device}, the current device is cuda:{d}")
+    return d
+
+
+def _raw_stream(stream, device: int):
+    if stream is not None:
+        return int(stream)
+    import torch
+    return torch._C._cuda_getCurrentRawStream(device)
+
+
+def _refuse(t, what: str, d: int, dtype, dim: int):
+    import torch
+    if not isinstance(t, torch.Tensor) or not t.is_cuda:
+        raise TypeError(f"{what} must be a device tensor")
+    if t.get_device() != d:
+        raise ValueError(f"{what} is on {t.device}, the current device is cuda:{d}")
+    if t.dtype is not dtype:
         raise TypeError(f"{what} must be {dtype}")
-    if dim is not None and t.dim() != dim:
-        raise TypeError(f"{what} must have {dim} dimensions")
+    raise TypeError(f"{what} must have {dim} dimensions")
 
 
-def _rows_of(t, what: str):
-    """Leading dimension of a 2-D tensor with unit column stride (a stride says
-    nothing where there is one row, or one column)."""
-    M, K = t.shape
+def _is(t, what: str, d: int, dtype, dim: int):
+    """A tensor of that type and number of dimensions on device d."""
+    try:
+        if t.get_device() == d and t.dtype is dtype and t.dim() == dim:
+            return
+    except AttributeError:
+        pass
+    _refuse(t, what, d, dtype, dim)
+
+
+def _vector(t, what: str, d: int, dtype, n: int) -> int:
+    """Address of a contiguous tensor of n elements."""
+    _is(t, what, d, dtype, 1)
+    if t.shape[0] != n or not t.is_contiguous():
+        raise ValueError(f"{what} must be a contiguous tensor of {n} elements")
+    return t.data_ptr()
+
+
+def _ld(t, what: str, M: int, K: int) -> int:
+    """Leading dimension of an [M, K] tensor with unit column stride (a stride
+    says nothing where there is one row, or one column)."""
     ld, unit = t.stride()
     if unit != 1 and K > 1:
         raise TypeError(f"{what} must have unit column stride")
-    if M > 1 and ld < K:
+    if M <= 1:
+        return ld if ld > K else K
+    if ld < K:
         raise TypeError(f"{what} has rows that overlap")
-    return ld if M > 1 else max(ld, K)
+    return ld
 
 
 def _type_of(t, what: str) -> int:
-    try:
-        return _types()[t.dtype]
-    except KeyError:
-        raise TypeError(f"{what} must be float32, bfloat16 or float16") from None
+    code = (_TYPES or _types()).get(t.dtype)
+    if code is None:
+        raise TypeError(f"{what} must be float32, bfloat16 or float16")
+    return code
 
 
 def soniq_quantize_rows(A, out=None, scales=None, stream=None):
@@ -554,44 +593,39 @@ def soniq_quantize_rows(A, out=None, scales=None, stream=None):
     float16 [M, K]) with one scale each: tokens, or the output channels of a
     weight matrix.  Returns (codes int8 [M, K], scales float32 [M])."""
     import torch
-    _here(A, "A", dim=2)
-    ta, lda = _type_of(A, "A"), _rows_of(A, "A")
+    d = _device(A, "A")
+    ta = _type_of(A, "A")
+    _is(A, "A", d, A.dtype, 2)
     M, K = A.shape
+    lda = _ld(A, "A", M, K)
     if out is None:
         out = torch.empty((M, -(-K // 16) * 16), dtype=torch.int8, device=A.device)[:, :K]
-    _here(out, "out", torch.int8, 2)
-    if tuple(out.shape) != (M, K):
-        raise ValueError("out must have A's shape")
+    else:
+        _is(out, "out", d, torch.int8, 2)
+        if out.shape != A.shape:
+            raise ValueError("out must have A's shape")
     if scales is None:
         scales = torch.empty(M, dtype=torch.float32, device=A.device)
-    _here(scales, "scales", torch.float32, 1)
-    if scales.shape[0] != M or not scales.is_contiguous():
-        raise ValueError("scales must be a contiguous [M] tensor")
-    _check(lib().soniq_quantize_rows(A.data_ptr(), ta, M, K, lda, out.data_ptr(), _rows_of(out, "out"),
-                                     scales.data_ptr(), _stream(stream)))
+    s = _vector(scales, "scales", d, torch.float32, M)
+    _check(lib().soniq_quantize_rows(A.data_ptr(), ta, M, K, lda, out.data_ptr(), _ld(out, "out", M, K), s,
+                                     _raw_stream(stream, d)))
     return out, scales
 
 
-def _weights_i8(W, s_w, bias, K, out, M, dtype, device):
+def _i8_operands(W, s_w, bias, d, M, K, out, dtype, device):
     import torch
-    _here(W, "W", torch.int8, 2)
-    N = W.shape[0]
-    if W.shape[1] != K:
+    _is(W, "W", d, torch.int8, 2)
+    N, Kw = W.shape
+    if Kw != K:
         raise ValueError("W has the wrong number of input channels")
-    _here(s_w, "s_w", torch.float32, 1)
-    if s_w.shape[0] != N or not s_w.is_contiguous():
-        raise ValueError("s_w must be a contiguous [N] tensor")
-    if bias is not None:
-        _here(bias, "bias", torch.float32, 1)
-        if bias.shape[0] != N or not bias.is_contiguous():
-            raise ValueError("bias must be a contiguous [N] tensor")
     if out is None:
         out = torch.empty((M, N), dtype=torch.bfloat16 if dtype is None else dtype, device=device)
     else:
-        _here(out, "out", dtype, 2)
-        if tuple(out.shape) != (M, N):
+        _is(out, "out", d, out.dtype if dtype is None else dtype, 2)
+        if out.shape[0] != M or out.shape[1] != N:
             raise ValueError("out must be [M, N]")
-    return N, out
+    return (N, W.data_ptr(), _ld(W, "W", N, K), _vector(s_w, "s_w", d, torch.float32, N),
+            None if bias is None else _vector(bias, "bias", d, torch.float32, N), out)
 
 
 def soniq_i8_gemm(A, s_a, W, s_w, bias=None, out=None, dtype=None, stream=None):
@@ -599,41 +633,50 @@ def soniq_i8_gemm(A, s_a, W, s_w, bias=None, out=None, dtype=None, stream=None):
     W [N, K] with float32 scales per row; Y [M, N] of `dtype` (bfloat16 unless
     given).  Returns Y."""
     import torch
-    _here(A, "A", torch.int8, 2)
+    d = _device(A, "A")
+    _is(A, "A", d, torch.int8, 2)
     M, K = A.shape
-    _here(s_a, "s_a", torch.float32, 1)
-    if s_a.shape[0] != M or not s_a.is_contiguous():
-        raise ValueError("s_a must be a contiguous [M] tensor")
-    N, out = _weights_i8(W, s_w, bias, K, out, M, dtype, A.device)
-    _check(lib().soniq_i8_gemm(A.data_ptr(), _rows_of(A, "A"), s_a.data_ptr(), W.data_ptr(),
-                               _rows_of(W, "W"), s_w.data_ptr(), None if bias is None else bias.data_ptr(),
-                               M, N, K, out.data_ptr(), _type_of(out, "out"), _rows_of(out, "out"),
-                               _stream(stream)))
+    sa = _vector(s_a, "s_a", d, torch.float32, M)
+    N, w, ldw, sw, b, out = _i8_operands(W, s_w, bias, d, M, K, out, dtype, A.device)
+    _check(lib().soniq_i8_gemm(A.data_ptr(), _ld(A, "A", M, K), sa, w, ldw, sw, b, M, N, K, out.data_ptr(),
+                               _type_of(out, "out"), _ld(out, "out", M, N), _raw_stream(stream, d)))
     return out
 
 
+@functools.lru_cache(maxsize=4096)
 def soniq_quantize_i8_gemm_workspace(M: int, K: int) -> int:
     n = ctypes.c_int64()
     _check(lib().soniq_quantize_i8_gemm_workspace(M, K, ctypes.byref(n)))
     return n.value
 
 
+def _work(work, need: int, d: int, device):
+    import torch
+    if work is None:
+        if need == 0:
+            return None, 0, None
+        work = torch.empty(need, dtype=torch.uint8, device=device)
+        return work.data_ptr(), need, work
+    _is(work, "work", d, torch.uint8, 1)
+    if not work.is_contiguous():
+        raise ValueError("work must be contiguous")
+    return work.data_ptr(), work.numel(), work
+
+
 def soniq_quantize_i8_gemm(A, W, s_w, bias=None, out=None, dtype=None, work=None, stream=None):
     """soniq_quantize_rows(A), then soniq_i8_gemm with W and s_w, in one call.
     work: a uint8 device tensor of soniq_quantize_i8_gemm_workspace(M, K)
     bytes (allocated when None).  Returns Y."""
-    import torch
-    _here(A, "A", dim=2)
-    ta, lda = _type_of(A, "A"), _rows_of(A, "A")
+    d = _device(A, "A")
+    ta = _type_of(A, "A")
+    _is(A, "A", d, A.dtype, 2)
     M, K = A.shape
-    N, out = _weights_i8(W, s_w, bias, K, out, M, dtype, A.device)
-    if work is None:
-        work = torch.empty(soniq_quantize_i8_gemm_workspace(M, K), dtype=torch.uint8, device=A.device)
-    _here(work, "work", torch.uint8, 1)
-    _check(lib().soniq_quantize_i8_gemm(A.data_ptr(), ta, lda, W.data_ptr(), _rows_of(W, "W"), s_w.data_ptr(),
-                                        None if bias is None else bias.data_ptr(), M, N, K, out.data_ptr(),
-                                        _type_of(out, "out"), _rows_of(out, "out"), work.data_ptr(),
-                                        work.numel(), _stream(stream)))
+    lda = _ld(A, "A", M, K)
+    N, w, ldw, sw, b, out = _i8_operands(W, s_w, bias, d, M, K, out, dtype, A.device)
+    wp, wn, work = _work(work, soniq_quantize_i8_gemm_workspace(M, K), d, A.device)
+    _check(lib().soniq_quantize_i8_gemm(A.data_ptr(), ta, lda, w, ldw, sw, b, M, N, K, out.data_ptr(),
+                                        _type_of(out, "out"), _ld(out, "out", M, N), wp, wn,
+                                        _raw_stream(stream, d)))
     return out
 
 
@@ -647,12 +690,13 @@ class KVCache:
 
     def __init__(self, k, k_scale, v, v_scale, bits: int = 8):
         import torch
+        d = _device(k, "k")
         for t, what in ((k, "k"), (v, "v")):
-            _here(t, what, dim=4)
+            _is(t, what, d, t.dtype, 4)
             if t.dtype not in (torch.int8, torch.uint8) or not t.is_contiguous():
                 raise TypeError(f"{what} must be a contiguous int8 or uint8 tensor")
         for t, what in ((k_scale, "k_scale"), (v_scale, "v_scale")):
-            _here(t, what, torch.float32, 3)
+            _is(t, what, d, torch.float32, 3)
             if not t.is_contiguous():
                 raise TypeError(f"{what} must be contiguous")
         if bits not in (4, 8):
@@ -662,44 +706,54 @@ class KVCache:
         self.k, self.k_scale, self.v, self.v_scale, self.bits = k, k_scale, v, v_scale, bits
         self.pages, self.heads, self.page_size, width = k.shape
         self.head_dim = width * 8 // bits
-        self.device = k.device
+        self.device, self.device_index = k.device, d
         self._c = KVCacheStruct(k.data_ptr(), k_scale.data_ptr(), v.data_ptr(), v_scale.data_ptr(),
                                 self.pages, self.page_size, self.heads, self.head_dim, bits)
         self._ref = ctypes.addressof(self._c)
 
     @classmethod
-    def empty(cls, pages: int, page_size: int, heads: int, head_dim: int, bits: int = 8, device=None):
-        """A cache of zeros."""
+    def empty(cls, pages: int, page_size: int, heads: int, head_dim: int, bits: int = 8):
+        """A cache of zeros on the current device."""
         import torch
-        device = torch.device("cuda", torch.cuda.current_device()) if device is None else device
+        if bits not in (4, 8) or head_dim * bits % 8:
+            raise ValueError("bits must be 4 or 8, and a row a whole number of bytes")
+        device = torch.device("cuda", torch.cuda.current_device())
         codes = lambda: torch.zeros((pages, heads, page_size, head_dim * bits // 8), dtype=torch.int8, device=device)  # noqa: E731
         scales = lambda: torch.zeros((pages, heads, page_size), dtype=torch.float32, device=device)  # noqa: E731
         return cls(codes(), scales(), codes(), scales(), bits)
 
 
 def _kv_batch(cache, page_table, cu, lengths, what):
+    """Device, and (B, width, leading dimension, addresses) of a ragged batch."""
     import torch
-    if cache.device.index != torch.cuda.current_device():
-        raise ValueError(f"the cache is on {cache.device}, the current device is cuda:{torch.cuda.current_device()}")
+    d = cache.device_index
+    if torch._C._cuda_getDevice() != d:
+        raise ValueError(f"the cache is on {cache.device}, the current device is another one")
     i32 = torch.int32
-    _here(page_table, "page_table", i32, 2)
-    _here(cu, "cu", i32, 1)
-    _here(lengths, what, i32, 1)
-    B = page_table.shape[0]
-    if cu.shape[0] != B + 1 or lengths.shape[0] != B or not cu.is_contiguous() or not lengths.is_contiguous():
-        raise ValueError(f"cu must be a contiguous [B + 1], {what} a contiguous [B] tensor")
-    return B, page_table.shape[1], _rows_of(page_table, "page_table")
+    _is(page_table, "page_table", d, i32, 2)
+    B, width = page_table.shape
+    return (d, B, width, _ld(page_table, "page_table", B, width), page_table.data_ptr(),
+            _vector(cu, "cu", d, i32, B + 1), _vector(lengths, what, d, i32, B))
 
 
-def _kv_rows(t, what: str, heads: int, head_dim: int):
+def _kv_rows(t, what: str, d: int, heads: int, head_dim: int):
     """Type code and strides of a [T, heads, head_dim] tensor."""
-    _here(t, what, dim=3)
-    if t.shape[1] != heads or t.shape[2] != head_dim:
+    code = _type_of(t, what)
+    _is(t, what, d, t.dtype, 3)
+    _, h, n = t.shape
+    if h != heads or n != head_dim:
         raise ValueError(f"{what} must be [T, {heads}, {head_dim}]")
     ts, hs, unit = t.stride()
     if unit != 1:
         raise TypeError(f"{what} must have unit stride in its last dimension")
-    return _type_of(t, what), ts, hs
+    return code, ts, hs
+
+
+def _kv_out(t, what: str, ts: int, hs: int):
+    """An output's rows must not overlap."""
+    T, heads, n = t.shape
+    if (T > 1 and ts < n) or (heads > 1 and hs < n):
+        raise TypeError(f"{what} has rows that overlap")
 
 
 def soniq_kv_write(cache: KVCache, K, V, page_table, cu, start, stream=None) -> None:
@@ -707,14 +761,14 @@ def soniq_kv_write(cache: KVCache, K, V, page_table, cu, start, stream=None) -> 
     cu[b] + i goes to position start[b] + i of sequence b, whose pages
     page_table[b] names.  page_table int32 [B, width], cu int32 [B + 1],
     start int32 [B], all on the device."""
-    B, width, ld = _kv_batch(cache, page_table, cu, start, "start")
-    tk, kts, khs = _kv_rows(K, "K", cache.heads, cache.head_dim)
-    tv, vts, vhs = _kv_rows(V, "V", cache.heads, cache.head_dim)
-    if tk != tv or K.shape[0] != V.shape[0]:
+    d, B, width, ld, table, cu, start = _kv_batch(cache, page_table, cu, start, "start")
+    tk, kts, khs = _kv_rows(K, "K", d, cache.heads, cache.head_dim)
+    tv, vts, vhs = _kv_rows(V, "V", d, cache.heads, cache.head_dim)
+    T = K.shape[0]
+    if tk != tv or T != V.shape[0]:
         raise ValueError("K and V must have one type and one number of tokens")
-    _check(lib().soniq_kv_write(cache._ref, K.data_ptr(), kts, khs, V.data_ptr(), vts, vhs, tk, K.shape[0],
-                                page_table.data_ptr(), ld, width, B, cu.data_ptr(), start.data_ptr(),
-                                _stream(stream)))
+    _check(lib().soniq_kv_write(cache._ref, K.data_ptr(), kts, khs, V.data_ptr(), vts, vhs, tk, T, table, ld, width,
+                                B, cu, start, _raw_stream(stream, d)))
 
 
 def soniq_kv_read(cache: KVCache, page_table, cu, start, tokens: int, dtype=None, out=None, stream=None):
@@ -723,27 +777,40 @@ def soniq_kv_read(cache: KVCache, page_table, cu, start, tokens: int, dtype=None
     unless given, or into the pair `out`).  Returns (K, V); rows from cu[B] on
     are left as they are (out=None: uninitialised)."""
     import torch
-    B, width, ld = _kv_batch(cache, page_table, cu, start, "start")
+    d, B, width, ld, table, cu, start = _kv_batch(cache, page_table, cu, start, "start")
+    heads, D = cache.heads, cache.head_dim
     if out is None:
-        kv = torch.empty((2, tokens, cache.heads, cache.head_dim),
-                         dtype=torch.bfloat16 if dtype is None else dtype, device=cache.device)
-        out = kv[0], kv[1]
-    K, V = out
-    tk, kts, khs = _kv_rows(K, "K", cache.heads, cache.head_dim)
-    tv, vts, vhs = _kv_rows(V, "V", cache.heads, cache.head_dim)
-    if tk != tv or K.shape[0] != tokens or V.shape[0] != tokens or (dtype is not None and K.dtype is not dtype):
-        raise ValueError("K and V must have one type (dtype) and `tokens` rows")
-    _check(lib().soniq_kv_read(cache._ref, K.data_ptr(), kts, khs, V.data_ptr(), vts, vhs, tk, tokens,
-                               page_table.data_ptr(), ld, width, B, cu.data_ptr(), start.data_ptr(),
-                               _stream(stream)))
+        dtype = torch.bfloat16 if dtype is None else dtype
+        K, V = torch.empty((2, tokens, heads, D), dtype=dtype, device=cache.device).unbind(0)
+        tk, kts, khs = _type_of(K, "dtype:"), heads * D, D
+        vts, vhs = kts, khs
+    else:
+        K, V = out
+        tk, kts, khs = _kv_rows(K, "K", d, heads, D)
+        tv, vts, vhs = _kv_rows(V, "V", d, heads, D)
+        if tk != tv or K.shape[0] != tokens or V.shape[0] != tokens or (dtype is not None and K.dtype is not dtype):
+            raise ValueError("K and V must have one type (dtype) and `tokens` rows")
+        _kv_out(K, "K", kts, khs)
+        _kv_out(V, "V", vts, vhs)
+    _check(lib().soniq_kv_read(cache._ref, K.data_ptr(), kts, khs, V.data_ptr(), vts, vhs, tk, tokens, table, ld,
+                               width, B, cu, start, _raw_stream(stream, d)))
     return K, V
+
+
+@functools.lru_cache(maxsize=4096)
+def _kv_work(pages, page_size, heads, head_dim, bits, tokens, q_heads, B, max_q, max_kv) -> int:
+    # the pointers say nothing about the size, but have to look like a cache's
+    c = KVCacheStruct(16, 16, 16, 16, pages, page_size, heads, head_dim, bits)
+    n = ctypes.c_int64()
+    _check(lib().soniq_kv_attention_workspace(ctypes.addressof(c), tokens, q_heads, B, max_q, max_kv,
+                                              ctypes.byref(n)))
+    return n.value
 
 
 def soniq_kv_attention_workspace(cache: KVCache, tokens: int, q_heads: int, B: int, max_q: int,
                                  max_kv: int) -> int:
-    n = ctypes.c_int64()
-    _check(lib().soniq_kv_attention_workspace(cache._ref, tokens, q_heads, B, max_q, max_kv, ctypes.byref(n)))
-    return n.value
+    return _kv_work(cache.pages, cache.page_size, cache.heads, cache.head_dim, cache.bits, tokens, q_heads, B,
+                    max_q, max_kv)
 
 
 def soniq_kv_attention(cache: KVCache, q, page_table, cu, kv_len, scale=None, mask=None, max_q=None,
@@ -759,38 +826,38 @@ def soniq_kv_attention(cache: KVCache, q, page_table, cu, kv_len, scale=None, ma
     work: a uint8 device tensor of soniq_kv_attention_workspace(...) bytes
     (allocated when None).  Returns out (like q)."""
     import torch
-    B, width, ld = _kv_batch(cache, page_table, cu, kv_len, "kv_len")
-    if q.dim() != 3:
-        raise TypeError("q must have 3 dimensions")
-    T, heads = q.shape[0], q.shape[1]
-    tq, qts, qhs = _kv_rows(q, "q", heads, cache.head_dim)
+    d, B, width, ld, table, cu, kv_len = _kv_batch(cache, page_table, cu, kv_len, "kv_len")
+    code = _type_of(q, "q")
+    _is(q, "q", d, q.dtype, 3)
+    T, heads, D = q.shape
+    qts, qhs, unit = q.stride()
+    if D != cache.head_dim or unit != 1:
+        raise ValueError(f"q must be [T, q_heads, {cache.head_dim}] with unit stride in its last dimension")
     if out is None:
-        out = torch.empty((T, heads, cache.head_dim), dtype=q.dtype, device=q.device)
-    to, ots, ohs = _kv_rows(out, "out", heads, cache.head_dim)
-    if to != tq or out.shape[0] != T:
-        raise ValueError("out must have q's shape and type")
-    words = 0
+        out = torch.empty((T, heads, D), dtype=q.dtype, device=cache.device)
+        ots, ohs = heads * D, D
+    else:
+        to, ots, ohs = _kv_rows(out, "out", d, heads, D)
+        if to != code or out.shape[0] != T:
+            raise ValueError("out must have q's shape and type")
+        _kv_out(out, "out", ots, ohs)
+    words, bits = 0, None
     if mask is not None:
-        _here(mask, "mask", torch.int64, 2)
+        _is(mask, "mask", d, torch.int64, 2)
         if mask.shape[0] != T or not mask.is_contiguous():
             raise ValueError("mask must be a contiguous [T, words] tensor")
-        words = mask.shape[1]
+        words, bits = mask.shape[1], mask.data_ptr()
     if lse is not None:
-        _here(lse, "lse", torch.float32, 2)
-        if tuple(lse.shape) != (T, heads) or not lse.is_contiguous():
+        _is(lse, "lse", d, torch.float32, 2)
+        if lse.shape[0] != T or lse.shape[1] != heads or not lse.is_contiguous():
             raise ValueError("lse must be a contiguous [T, q_heads] tensor")
     if max_q is None:
         max_q = max(T, 1)
     if max_kv is None:
         max_kv = width * cache.page_size
-    if work is None:
-        work = torch.empty(soniq_kv_attention_workspace(cache, T, heads, B, max_q, max_kv), dtype=torch.uint8,
-                           device=q.device)
-    _here(work, "work", torch.uint8, 1)
-    _check(lib().soniq_kv_attention(cache._ref, q.data_ptr(), qts, qhs, tq, T, heads, page_table.data_ptr(), ld,
-                                    width, B, cu.data_ptr(), kv_len.data_ptr(),
-                                    None if mask is None else mask.data_ptr(), words,
-                                    cache.head_dim ** -0.5 if scale is None else scale, max_q, max_kv,
-                                    out.data_ptr(), ots, ohs, None if lse is None else lse.data_ptr(),
-                                    work.data_ptr(), work.numel(), _stream(stream)))
+    wp, wn, work = _work(work, soniq_kv_attention_workspace(cache, T, heads, B, max_q, max_kv), d, cache.device)
+    _check(lib().soniq_kv_attention(cache._ref, q.data_ptr(), qts, qhs, code, T, heads, table, ld, width, B, cu,
+                                    kv_len, bits, words, D ** -0.5 if scale is None else scale, max_q, max_kv,
+                                    out.data_ptr(), ots, ohs, None if lse is None else lse.data_ptr(), wp, wn,
+                                    _raw_stream(stream, d)))
     return out
