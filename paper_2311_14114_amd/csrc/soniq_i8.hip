@@ -10,6 +10,7 @@
 #include "soniq_values.h"
 
 #include <algorithm>
+#include <type_traits>
 
 namespace soniq {
 namespace {
@@ -247,19 +248,24 @@ __global__ __launch_bounds__(512) void k_i8_skinny(I8Gemm g) {
 
 // ----------------------------------------------------------- many tokens --
 // BM x BN tile, four waves of (BM/2) x (BN/2), 128 channels a stage through
-// two LDS buffers.  Rows go from memory to registers one stage ahead and
-// into LDS half a stage ahead, so that any alignment, any bound and the last
-// partial stage are a matter of that load alone.  LDS rows are 128 bytes;
+// two LDS buffers.  Rows go from memory to registers one stage ahead, so that
+// any alignment and the last partial stage are a matter of that load alone,
+// and into LDS within the stage before their own.  LDS rows are 128 bytes;
 // the 16-byte chunk c of row r sits at chunk c ^ (r / 2 % 8), which spreads
-// the 16 rows that a fragment read touches at once over all banks.  Within a
-// stage the fragments of the next 32 channels are read before the products
-// of these, across the barrier too.
-// Off: type of a row's offset in its tile (64 bits for row strides of 2^24
-// bytes and more).
-template <int BM, int BN, class Off>
+// the 16 rows that a fragment read touches at once over all banks.
+// A stage has four steps of 32 channels: the fragments of the next step are
+// read during the products of this one, across the barrier too, and the
+// first three steps each move a third of the next stage into LDS and load
+// that third of the one after.
+//
+// A tile that would pass the last row or channel starts earlier instead (its
+// neighbour computes the same outputs, to the same bits).  CLAMP: for
+// matrices smaller than a tile, and for row strides of 2^24 bytes and more:
+// each row's address by itself.
+template <int BM, int BN, bool CLAMP>
 __global__ __launch_bounds__(256, BM * BN > 128 * 128 ? 1 : 2) void k_i8_tile(I8Gemm g, int tm, int tn) {
   constexpr int TM = BM / 64, TN = BN / 64;        // 32x32 tiles a wave
-  constexpr int LA = BM / 32, LB = BN / 32;        // 16-byte loads a thread and stage
+  constexpr int LA = BM / 32, LB = BN / 32, NS = LA + LB;  // 16-byte loads a thread and stage
   __shared__ __align__(16) int8_t lds[2][(BM + BN) * 128];
 
   // Workgroup b runs on XCD b % 8: each XCD takes a contiguous run of the
@@ -276,29 +282,29 @@ __global__ __launch_bounds__(256, BM * BN > 128 * 128 ? 1 : 2) void k_i8_tile(I8
   }
   const int tid = threadIdx.x, lane = tid % 64;
   const int wave = __builtin_amdgcn_readfirstlane(tid / 64);
-  const int64_t m0 = (int64_t)bm * BM, n0 = (int64_t)bn * BN;
+  const int64_t m0 = CLAMP ? (int64_t)bm * BM : min((int64_t)bm * BM, g.M - BM);
+  const int64_t n0 = CLAMP ? (int64_t)bn * BN : min((int64_t)bn * BN, g.N - BN);
   const int lr = tid / 8, lc = tid % 8;
-  const int8_t *ta = g.A + m0 * g.lda, *tb = g.W + n0 * g.ldw;
-  Off oa[LA], ob[LB];
-#pragma unroll
-  for (int i = 0; i < LA; ++i) oa[i] = (Off)(min((int64_t)(lr + 32 * i), g.M - 1 - m0) * g.lda) + 16 * lc;
-#pragma unroll
-  for (int i = 0; i < LB; ++i) ob[i] = (Off)(min((int64_t)(lr + 32 * i), g.N - 1 - n0) * g.ldw) + 16 * lc;
-  v4i ra[LA], rb[LB];
   const int stages = (int)((g.K + 127) / 128);
   const bool tail = g.K % 128 != 0;
   // In a partial last stage, chunks that cross the end of a row are taken from
   // its last 16 bytes (K >= 16 here) and moved down when they are written;
   // `over`: how many bytes past the end this thread's chunk would reach.
   const int over = max(0, 16 * lc + 16 - (int)(g.K - (int64_t)(stages - 1) * 128));
-  auto load = [&](int s) {
-    const int64_t k = (int64_t)s * 128 - 128;
-    const int at = 128 - (s == stages - 1 ? over : 0);  // 1 .. 128
+  const int8_t* row[NS];  // uniform without CLAMP
 #pragma unroll
-    for (int i = 0; i < LA; ++i) ra[i] = load16(ta + k + (oa[i] + at));
-#pragma unroll
-    for (int i = 0; i < LB; ++i) rb[i] = load16(tb + k + (ob[i] + at));
-  };
+  for (int i = 0; i < NS; ++i) {
+    const bool isA = i < LA;
+    const int r = 32 * (isA ? i : i - LA);
+    if constexpr (CLAMP)
+      row[i] = isA ? g.A + min(m0 + lr + r, g.M - 1) * g.lda : g.W + min(n0 + lr + r, g.N - 1) * g.ldw;
+    else
+      row[i] = isA ? g.A + (m0 + r) * g.lda : g.W + (n0 + r) * g.ldw;
+  }
+  const uint32_t va = (CLAMP ? 0 : (uint32_t)(lr * g.lda)) + 16 * lc, vb = (CLAMP ? 0 : (uint32_t)(lr * g.ldw)) + 16 * lc;
+  v4i st[NS];
+  // k: byte of the rows where the stage starts (this thread's chunk is 16 lc further)
+  auto load = [&](int i, uint32_t k) { st[i] = load16(row[i] + ((i < LA ? va : vb) + k)); };
   auto move_down = [&](v4i& x) {
     const uint64_t lo = (uint32_t)x[0] | (uint64_t)(uint32_t)x[1] << 32;
     const uint64_t hi = (uint32_t)x[2] | (uint64_t)(uint32_t)x[3] << 32;
@@ -309,19 +315,7 @@ __global__ __launch_bounds__(256, BM * BN > 128 * 128 ? 1 : 2) void k_i8_tile(I8
     x[2] = over >= 16 ? 0 : (int)h, x[3] = over >= 16 ? 0 : (int)(h >> 32);
   };
   const int wat = lr * 128 + ((lc ^ (lr / 2 % 8)) << 4);
-  auto write = [&](int buf, int s) {
-    if (tail && s == stages - 1) {
-      asm volatile("");  // a branch, not selects in every stage
-#pragma unroll
-      for (int i = 0; i < LA; ++i) move_down(ra[i]);
-#pragma unroll
-      for (int i = 0; i < LB; ++i) move_down(rb[i]);
-    }
-#pragma unroll
-    for (int i = 0; i < LA; ++i) *reinterpret_cast<v4i*>(&lds[buf][wat + 4096 * i]) = ra[i];
-#pragma unroll
-    for (int i = 0; i < LB; ++i) *reinterpret_cast<v4i*>(&lds[buf][BM * 128 + wat + 4096 * i]) = rb[i];
-  };
+  auto write = [&](int i, int buf) { *reinterpret_cast<v4i*>(&lds[buf][wat + 4096 * i]) = st[i]; };
   const int wm = (wave & 1) * (BM / 2), wn = (wave >> 1) * (BN / 2);
   int rat[4];
 #pragma unroll
@@ -351,29 +345,84 @@ __global__ __launch_bounds__(256, BM * BN > 128 * 128 ? 1 : 2) void k_i8_tile(I8
       for (int j = 0; j < TN; ++j)
         acc[i][j] = __builtin_amdgcn_mfma_i32_32x32x32_i8(x.a[i], x.b[j], acc[i][j], 0, 0, 0);
   };
+  // What a step issues beside its products, one piece after each product:
+  // fragment reads first (the next step waits for them), then LDS writes
+  // with the loads that refill their registers.
+  auto interleave = [&](auto moved) {
+    constexpr int kMoved = decltype(moved)::value, kReads = TM + TN, kMma = TM * TN;
+    constexpr int kPer = (kReads + 2 * kMoved + kMma - 1) / kMma;
+#pragma unroll
+    for (int i = 0; i < kMma; ++i) {
+      __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+      if (i * kPer < kReads) {
+        __builtin_amdgcn_sched_group_barrier(0x100, kPer, 0);
+      } else {
+        __builtin_amdgcn_sched_group_barrier(0x200, (kPer + 1) / 2, 0);
+        __builtin_amdgcn_sched_group_barrier(0x020, (kPer + 1) / 2, 0);
+      }
+    }
+    __builtin_amdgcn_sched_barrier(0);
+  };
+  constexpr int kCut[4] = {0, (NS + 2) / 3, (NS + 2) / 3 + (NS + 1) / 3, NS};
 
-  load(0);
-  write(0, 0);
-  if (stages > 1) load(1);
+#pragma unroll
+  for (int i = 0; i < NS; ++i) load(i, stages == 1 ? (uint32_t)-over : 0u);
+  if (stages == 1 && tail) {
+#pragma unroll
+    for (int i = 0; i < NS; ++i) move_down(st[i]);
+  }
+#pragma unroll
+  for (int i = 0; i < NS; ++i) write(i, 0);
+  if (stages > 1) {
+#pragma unroll
+    for (int i = 0; i < NS; ++i) load(i, 128u - (stages == 2 ? over : 0));
+  }
   lds_barrier();
   read(f[0], 0, 0);
-  for (int s = 0; s < stages; ++s) {
+  int s = 0;
+  for (; s + 3 < stages; ++s) {
+    const int buf = s & 1;
+    const uint32_t k = (uint32_t)(s + 2) * 128;
+#pragma unroll
+    for (int ks = 0; ks < 3; ++ks) {
+      read(f[(ks + 1) & 1], buf, ks + 1);
+      mma(f[ks & 1]);
+#pragma unroll
+      for (int i = 0; i < NS; ++i)
+        if (i >= kCut[ks] && i < kCut[ks + 1]) write(i, buf ^ 1), load(i, k);
+      interleave(std::integral_constant<int, (NS + 2) / 3>());
+    }
+    lds_barrier();
+    read(f[0], buf ^ 1, 0);
+    mma(f[1]);
+    interleave(std::integral_constant<int, 0>());
+  }
+  // the last three stages: nothing to load any more, and perhaps a partial one
+  for (; s < stages; ++s) {
     const int buf = s & 1;
     read(f[1], buf, 1);
     mma(f[0]);
-    __builtin_amdgcn_sched_barrier(0);
     read(f[0], buf, 2);
     mma(f[1]);
-    __builtin_amdgcn_sched_barrier(0);
     read(f[1], buf, 3);
-    if (s + 1 < stages) write(buf ^ 1, s + 1);
-    if (s + 2 < stages) load(s + 2);
+    if (tail && s + 1 == stages - 1) {
+      asm volatile("");  // a branch, not selects
+#pragma unroll
+      for (int i = 0; i < NS; ++i) move_down(st[i]);
+    }
+    if (s + 1 < stages) {
+#pragma unroll
+      for (int i = 0; i < NS; ++i) write(i, buf ^ 1);
+    }
+    if (s + 2 < stages) {
+      const uint32_t k = (uint32_t)(s + 2) * 128 - (s + 2 == stages - 1 ? over : 0);
+#pragma unroll
+      for (int i = 0; i < NS; ++i) load(i, k);
+    }
     mma(f[0]);
-    __builtin_amdgcn_sched_barrier(0);
     lds_barrier();
     if (s + 1 < stages) read(f[0], buf ^ 1, 0);
     mma(f[1]);
-    __builtin_amdgcn_sched_barrier(0);
   }
 
 #pragma unroll
@@ -419,10 +468,10 @@ void launch_rows(const void* A, int64_t M, int64_t K, int64_t lda, int8_t* Q, in
   }
 }
 
-template <int BM, int BN, class Off>
+template <int BM, int BN, bool CLAMP>
 void launch_tile(const I8Gemm& g, hipStream_t stream) {
   const int64_t tm = (g.M + BM - 1) / BM, tn = (g.N + BN - 1) / BN;
-  k_i8_tile<BM, BN, Off><<<(unsigned)((tm * tn + 7) / 8 * 8), 256, 0, stream>>>(g, (int)tm, (int)tn);
+  k_i8_tile<BM, BN, CLAMP><<<(unsigned)((tm * tn + 7) / 8 * 8), 256, 0, stream>>>(g, (int)tm, (int)tn);
 }
 
 template <int MT>
@@ -449,10 +498,10 @@ hipError_t launch_i8_gemm(const I8Gemm& g, hipStream_t stream) {
   else if (g.M <= 48) launch_skinny<3>(g, stream);
   else if (g.M <= 64) launch_skinny<4>(g, stream);
   else if (g.K < 16) k_i8_short<<<dim3((unsigned)((g.N + 255) / 256), (unsigned)std::min<int64_t>(g.M, 65535)), 256, 0, stream>>>(g);
-  else if (std::max(g.lda, g.ldw) >= 1 << 24) launch_tile<64, 64, uint64_t>(g, stream);
-  else if (((g.M + 255) / 256) * ((g.N + 255) / 256) >= 200) launch_tile<256, 256, uint32_t>(g, stream);
-  else if (((g.M + 127) / 128) * ((g.N + 127) / 128) >= 200) launch_tile<128, 128, uint32_t>(g, stream);
-  else launch_tile<64, 64, uint32_t>(g, stream);
+  else if (std::max(g.lda, g.ldw) >= 1 << 24 || g.N < 64) launch_tile<64, 64, true>(g, stream);
+  else if (((g.M + 255) / 256) * ((g.N + 255) / 256) >= 200 && std::min(g.M, g.N) >= 256) launch_tile<256, 256, false>(g, stream);
+  else if (((g.M + 127) / 128) * ((g.N + 127) / 128) >= 200 && std::min(g.M, g.N) >= 128) launch_tile<128, 128, false>(g, stream);
+  else launch_tile<64, 64, false>(g, stream);
   return hipGetLastError();
 }
 
