@@ -247,6 +247,77 @@ __global__ __launch_bounds__(512) void k_i8_skinny(I8Gemm g) {
 }
 
 // ----------------------------------------------------------- many tokens --
+// A wave's outputs, scaled and stored.  Lane (c, hi) holds row m = c of each
+// 32x32 tile, and of it columns 8 g + 4 hi + e: four neighbours, packed into
+// this wave's part of LDS as one piece; 32 rows at a time then leave in whole
+// 16-byte pieces of consecutive columns.
+template <int TYPE, int TM, int TN, bool CLAMP>
+__device__ __forceinline__ void tile_out(const I8Gemm& g, const v16i (&acc)[TM][TN], int8_t* lds, int64_t mw,
+                                         int64_t nw, int lane) {
+  typedef typename Value<TYPE>::T T;
+  constexpr int E = sizeof(T), kCols = 32 * TN, kPitch = kCols * E + 16;  // bytes of a row in LDS
+  constexpr int kLanes = kCols * E / 16;                                  // lanes a row on the way out
+  const int c = lane % 32, hi = lane / 32;
+  struct __attribute__((packed, aligned(4))) F4 { float v[4]; };
+  float sw[TN][4][4];
+#pragma unroll
+  for (int j = 0; j < TN; ++j)
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      const int64_t n = nw + 32 * j + 8 * q + 4 * hi;
+      if constexpr (CLAMP) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) sw[j][q][e] = g.sw[min(n + e, g.N - 1)];
+      } else {
+        const F4 x = *reinterpret_cast<const F4*>(g.sw + n);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) sw[j][q][e] = x.v[e];
+      }
+    }
+#pragma unroll
+  for (int i = 0; i < TM; ++i) {
+    const int64_t m = mw + 32 * i + c;
+    const float sa = g.sa[CLAMP ? min(m, g.M - 1) : m];
+#pragma unroll
+    for (int j = 0; j < TN; ++j)
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        T y[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          float v = scaled(acc[i][j][4 * q + e], sa, sw[j][q][e]);
+          if (g.bias) {
+            const int64_t n = nw + 32 * j + 8 * q + 4 * hi + e;
+            v = __fadd_rn(v, g.bias[CLAMP ? min(n, g.N - 1) : n]);
+          }
+          y[e] = Value<TYPE>::store(v);
+        }
+        __builtin_memcpy(lds + c * kPitch + (32 * j + 8 * q + 4 * hi) * E, y, sizeof y);
+      }
+    // the wave's own region: its stores above come before its loads below
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront", "local");
+#pragma unroll
+    for (int r0 = 0; r0 < 32; r0 += 64 / kLanes) {
+      const int r = r0 + lane / kLanes, col = lane % kLanes * (16 / E);
+      struct __attribute__((packed, aligned(E))) P { T v[16 / E]; };
+      P x;
+      __builtin_memcpy(&x, __builtin_assume_aligned(lds + r * kPitch + col * E, 16), 16);
+      const int64_t my = mw + 32 * i + r, ny = nw + col;
+      T* out = static_cast<T*>(g.Y) + my * g.ldy + ny;
+      if constexpr (CLAMP) {
+        if (my < g.M) {
+#pragma unroll
+          for (int e = 0; e < 16 / E; ++e)
+            if (ny + e < g.N) out[e] = x.v[e];
+        }
+      } else {
+        *reinterpret_cast<P*>(out) = x;
+      }
+    }
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront", "local");
+  }
+}
+
 // BM x BN tile, four waves of (BM/2) x (BN/2), 128 channels a stage through
 // two LDS buffers.  Rows go from memory to registers one stage ahead, so that
 // any alignment and the last partial stage are a matter of that load alone,
@@ -343,7 +414,7 @@ __global__ __launch_bounds__(256, BM * BN > 128 * 128 ? 1 : 2) void k_i8_tile(I8
     for (int i = 0; i < TM; ++i)
 #pragma unroll
       for (int j = 0; j < TN; ++j)
-        acc[i][j] = __builtin_amdgcn_mfma_i32_32x32x32_i8(x.a[i], x.b[j], acc[i][j], 0, 0, 0);
+        acc[i][j] = __builtin_amdgcn_mfma_i32_32x32x32_i8(x.b[j], x.a[i], acc[i][j], 0, 0, 0);
   };
   // What a step issues beside its products, one piece after each product:
   // fragment reads first (the next step waits for them), then LDS writes
@@ -425,21 +496,12 @@ __global__ __launch_bounds__(256, BM * BN > 128 * 128 ? 1 : 2) void k_i8_tile(I8
     mma(f[1]);
   }
 
-#pragma unroll
-  for (int j = 0; j < TN; ++j) {
-    const int64_t n = n0 + wn + 32 * j + lane % 32;
-    const float sw = n < g.N ? g.sw[n] : 0.0f, bias = g.bias && n < g.N ? g.bias[n] : 0.0f;
-#pragma unroll
-    for (int i = 0; i < TM; ++i)
-#pragma unroll
-      for (int e = 0; e < 16; ++e) {
-        const int64_t m = m0 + wm + 32 * i + 8 * (e / 4) + 4 * (lane / 32) + e % 4;
-        if (m >= g.M || n >= g.N) continue;
-        float y = scaled(acc[i][j][e], g.sa[m], sw);
-        if (g.bias) y = __fadd_rn(y, bias);
-        store_y(g, m * g.ldy + n, y);
-      }
-  }
+  __syncthreads();  // the outputs go through the same LDS
+  int8_t* mine = &lds[0][0] + wave * (int)(sizeof lds / 4);
+  const int64_t mw = m0 + wm, nw = n0 + wn;
+  if (g.y_type == SONIQ_BF16) tile_out<SONIQ_BF16, TM, TN, CLAMP>(g, acc, mine, mw, nw, lane);
+  else if (g.y_type == SONIQ_F16) tile_out<SONIQ_F16, TM, TN, CLAMP>(g, acc, mine, mw, nw, lane);
+  else tile_out<SONIQ_F32, TM, TN, CLAMP>(g, acc, mine, mw, nw, lane);
 }
 
 // Many tokens of fewer than 16 channels: one output a thread.
