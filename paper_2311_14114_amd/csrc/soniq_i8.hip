@@ -165,9 +165,8 @@ __device__ __forceinline__ float scaled(int acc, float sa, float sw) {
 // ------------------------------------------------------------ few tokens --
 // A workgroup of eight waves takes 16 * NT output channels and all tokens
 // (at most 16 * MT); wave w takes the 128-byte segments w, w + 8, ... of K.
-// A lane loads 32 bytes of its row per segment, q = lane / 16 choosing which:
-// the two products of a segment then see k in the order
-// 32 q + 16 j + i on both sides, which is as good as any.  Sums meet in LDS.
+// A load takes 16 bytes a lane, 64 neighbouring bytes of each of 16 rows: an
+// operand of the product as it is.  Sums meet in LDS.
 template <int MT, int NT>
 __global__ __launch_bounds__(512) void k_i8_skinny(I8Gemm g) {
   constexpr int U = MT * NT == 1 ? 4 : MT + NT <= 3 ? 3 : 2;  // segments in flight
@@ -177,9 +176,9 @@ __global__ __launch_bounds__(512) void k_i8_skinny(I8Gemm g) {
   const int64_t n0 = (int64_t)blockIdx.x * (16 * NT);
   const int8_t *wr[NT], *ar[MT];
 #pragma unroll
-  for (int j = 0; j < NT; ++j) wr[j] = g.W + min(n0 + 16 * j + r, g.N - 1) * g.ldw + 32 * q;
+  for (int j = 0; j < NT; ++j) wr[j] = g.W + min(n0 + 16 * j + r, g.N - 1) * g.ldw + 16 * q;
 #pragma unroll
-  for (int i = 0; i < MT; ++i) ar[i] = g.A + min((int64_t)(16 * i + r), g.M - 1) * g.lda + 32 * q;
+  for (int i = 0; i < MT; ++i) ar[i] = g.A + min((int64_t)(16 * i + r), g.M - 1) * g.lda + 16 * q;
   v4i acc[MT][NT] = {};
   const int full = (int)(g.K / 128);
   auto mma = [&](const v4i (&w)[NT][2], const v4i (&a)[MT][2]) {
@@ -198,9 +197,9 @@ __global__ __launch_bounds__(512) void k_i8_skinny(I8Gemm g) {
     for (int u = 0; u < U; ++u) {
       const int64_t k = (int64_t)(sgm + 8 * u) * 128;
 #pragma unroll
-      for (int j = 0; j < NT; ++j) w[u][j][0] = load16(wr[j] + k), w[u][j][1] = load16(wr[j] + k + 16);
+      for (int j = 0; j < NT; ++j) w[u][j][0] = load16(wr[j] + k), w[u][j][1] = load16(wr[j] + k + 64);
 #pragma unroll
-      for (int i = 0; i < MT; ++i) a[u][i][0] = load16(ar[i] + k), a[u][i][1] = load16(ar[i] + k + 16);
+      for (int i = 0; i < MT; ++i) a[u][i][0] = load16(ar[i] + k), a[u][i][1] = load16(ar[i] + k + 64);
     }
 #pragma unroll
     for (int u = 0; u < U; ++u) mma(w[u], a[u]);
@@ -209,20 +208,20 @@ __global__ __launch_bounds__(512) void k_i8_skinny(I8Gemm g) {
     const int64_t k = (int64_t)sgm * 128;
     v4i w[NT][2], a[MT][2];
 #pragma unroll
-    for (int j = 0; j < NT; ++j) w[j][0] = load16(wr[j] + k), w[j][1] = load16(wr[j] + k + 16);
+    for (int j = 0; j < NT; ++j) w[j][0] = load16(wr[j] + k), w[j][1] = load16(wr[j] + k + 64);
 #pragma unroll
-    for (int i = 0; i < MT; ++i) a[i][0] = load16(ar[i] + k), a[i][1] = load16(ar[i] + k + 16);
+    for (int i = 0; i < MT; ++i) a[i][0] = load16(ar[i] + k), a[i][1] = load16(ar[i] + k + 64);
     mma(w, a);
   }
   if (g.K % 128 && wave == full % 8) {
-    const int64_t k = (int64_t)full * 128 + 32 * q;
+    const int64_t k = (int64_t)full * 128 + 16 * q;
     v4i w[NT][2], a[MT][2];
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
 #pragma unroll
-      for (int j = 0; j < NT; ++j) w[j][h] = load16_to(wr[j] - 32 * q, k + 16 * h, g.K);
+      for (int j = 0; j < NT; ++j) w[j][h] = load16_to(wr[j] - 16 * q, k + 64 * h, g.K);
 #pragma unroll
-      for (int i = 0; i < MT; ++i) a[i][h] = load16_to(ar[i] - 32 * q, k + 16 * h, g.K);
+      for (int i = 0; i < MT; ++i) a[i][h] = load16_to(ar[i] - 16 * q, k + 64 * h, g.K);
     }
     mma(w, a);
   }
@@ -251,7 +250,7 @@ __global__ __launch_bounds__(512) void k_i8_skinny(I8Gemm g) {
 // 32x32 tile, and of it columns 8 g + 4 hi + e: four neighbours, packed into
 // this wave's part of LDS as one piece; 32 rows at a time then leave in whole
 // 16-byte pieces of consecutive columns.
-template <int TYPE, int TM, int TN, bool CLAMP>
+template <int TYPE, bool BIAS, int TM, int TN, bool CLAMP>
 __device__ __forceinline__ void tile_out(const I8Gemm& g, const v16i (&acc)[TM][TN], int8_t* lds, int64_t mw,
                                          int64_t nw, int lane) {
   typedef typename Value<TYPE>::T T;
@@ -286,7 +285,7 @@ __device__ __forceinline__ void tile_out(const I8Gemm& g, const v16i (&acc)[TM][
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
           float v = scaled(acc[i][j][4 * q + e], sa, sw[j][q][e]);
-          if (g.bias) {
+          if constexpr (BIAS) {
             const int64_t n = nw + 32 * j + 8 * q + 4 * hi + e;
             v = __fadd_rn(v, g.bias[CLAMP ? min(n, g.N - 1) : n]);
           }
@@ -499,9 +498,14 @@ __global__ __launch_bounds__(256, BM * BN > 128 * 128 ? 1 : 2) void k_i8_tile(I8
   __syncthreads();  // the outputs go through the same LDS
   int8_t* mine = &lds[0][0] + wave * (int)(sizeof lds / 4);
   const int64_t mw = m0 + wm, nw = n0 + wn;
-  if (g.y_type == SONIQ_BF16) tile_out<SONIQ_BF16, TM, TN, CLAMP>(g, acc, mine, mw, nw, lane);
-  else if (g.y_type == SONIQ_F16) tile_out<SONIQ_F16, TM, TN, CLAMP>(g, acc, mine, mw, nw, lane);
-  else tile_out<SONIQ_F32, TM, TN, CLAMP>(g, acc, mine, mw, nw, lane);
+  auto out = [&](auto type) {
+    constexpr int T = decltype(type)::value;
+    if (g.bias) tile_out<T, true, TM, TN, CLAMP>(g, acc, mine, mw, nw, lane);
+    else tile_out<T, false, TM, TN, CLAMP>(g, acc, mine, mw, nw, lane);
+  };
+  if (g.y_type == SONIQ_BF16) out(std::integral_constant<int, SONIQ_BF16>());
+  else if (g.y_type == SONIQ_F16) out(std::integral_constant<int, SONIQ_F16>());
+  else out(std::integral_constant<int, SONIQ_F32>());
 }
 
 // Many tokens of fewer than 16 channels: one output a thread.
