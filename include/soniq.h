@@ -552,9 +552,9 @@ soniq_status soniq_i8_gemm(const int8_t* A_dev, int64_t lda, const float* s_a_de
  * the codes and scales in the caller's workspace (a few tokens take one
  * launch).  Results are bit-identical to the two calls.
  *   work_dev    device, 16-byte aligned, at least the bytes that
- *               soniq_quantize_i8_gemm_workspace gives for (M, K); holds
- *               nothing between calls, and calls that may overlap need one
- *               each
+ *               soniq_quantize_i8_gemm_workspace gives for (M, K) (NULL
+ *               where that is 0); holds nothing between calls, and calls
+ *               that may overlap need one each
  * The other arguments and errors are those of the two calls.
  */
 soniq_status soniq_quantize_i8_gemm(const void* A_dev, int a_type, int64_t lda,
@@ -618,8 +618,8 @@ soniq_status soniq_kv_write(const soniq_kv_cache_t* cache, const void* K_dev,
                             void* stream);
 
 /*
- * soniq_kv_read -- the values of cached positions (code * scale, rounded
- * once to `type`): position start[b] + i of sequence b into row cu[b] + i
+ * soniq_kv_read -- the values of cached positions (code * scale in fp32, then
+ * rounded to `type`): position start[b] + i of sequence b into row cu[b] + i
  * of K and V [T, heads, head_dim].  Arguments and errors as soniq_kv_write.
  */
 soniq_status soniq_kv_read(const soniq_kv_cache_t* cache, void* K_dev, int64_t k_token_stride,

@@ -155,7 +155,7 @@ __global__ __launch_bounds__(256) void k_rows(const typename Value<TYPE>::T* A, 
 // --------------------------------------------------------------- outputs --
 __device__ __forceinline__ void store_y(const I8Gemm& g, int64_t at, float y) {
   if (g.y_type == SONIQ_BF16) static_cast<uint16_t*>(g.Y)[at] = bf16_bits(y);
-  else if (g.y_type == SONIQ_F16) static_cast<_Float16*>(g.Y)[at] = (_Float16)y;
+  else if (g.y_type == SONIQ_F16) static_cast<_Float16*>(g.Y)[at] = Value<SONIQ_F16>::store(y);
   else static_cast<float*>(g.Y)[at] = y;
 }
 __device__ __forceinline__ float scaled(int acc, float sa, float sw) {
@@ -164,84 +164,232 @@ __device__ __forceinline__ float scaled(int acc, float sa, float sw) {
 
 // ------------------------------------------------------------ few tokens --
 // A workgroup of eight waves takes 16 * NT output channels and all tokens
-// (at most 16 * MT); wave w takes the 128-byte segments w, w + 8, ... of K.
-// A load takes 16 bytes a lane, 64 neighbouring bytes of each of 16 rows: an
-// operand of the product as it is.  Sums meet in LDS.
-template <int MT, int NT>
+// (at most 8 * A8); wave w takes the 128-byte segments w, w + 8, ... of K.  A
+// load takes whole 128-byte pieces of 8 rows: a cache serves neighbouring
+// lanes of one line at once, but an operand of the product has neighbouring
+// lanes in different rows (loading operands as they are took 60 accesses an
+// instruction and half the speed).  So each wave turns its segments through
+// its own part of LDS, with no barrier; sums meet in LDS at the end.
+template <int A8, int NT>
 __global__ __launch_bounds__(512) void k_i8_skinny(I8Gemm g) {
-  constexpr int U = MT * NT == 1 ? 4 : MT + NT <= 3 ? 3 : 2;  // segments in flight
-  __shared__ int red[8][MT * NT][4][64];
+  constexpr int MT = (A8 + 1) / 2, NL = A8 + 2 * NT;           // loads a lane and segment
+  constexpr int U = NL <= 3 ? 4 : NL <= 6 ? 2 : 1;             // segments in flight
+  constexpr int kWave = (16 * MT + 16 * NT) * 128;             // LDS bytes of a wave
+  constexpr int kRed = 8 * MT * NT * 256 * 4;
+  __shared__ __align__(16) int8_t lds[8 * kWave > kRed ? 8 * kWave : kRed];
   const int tid = threadIdx.x, lane = tid % 64, r = lane % 16, q = lane / 16;
   const int wave = __builtin_amdgcn_readfirstlane(tid / 64);
   const int64_t n0 = (int64_t)blockIdx.x * (16 * NT);
-  const int8_t *wr[NT], *ar[MT];
+  const int lr = lane / 8, lc = lane % 8;
+  const int8_t* row[NL];
 #pragma unroll
-  for (int j = 0; j < NT; ++j) wr[j] = g.W + min(n0 + 16 * j + r, g.N - 1) * g.ldw + 16 * q;
-#pragma unroll
-  for (int i = 0; i < MT; ++i) ar[i] = g.A + min((int64_t)(16 * i + r), g.M - 1) * g.lda + 16 * q;
+  for (int i = 0; i < NL; ++i)
+    row[i] = i < A8 ? g.A + min((int64_t)(8 * i + lr), g.M - 1) * g.lda
+                    : g.W + min(n0 + 8 * (i - A8) + lr, g.N - 1) * g.ldw;
+  // rows 0 .. 16 MT - 1 of the wave's LDS are tokens (those past 8 * A8 hold
+  // anything: their sums are not stored), then 16 NT channels; chunk c of row
+  // x at c ^ (x / 2 % 8), as in the tiles below
+  int8_t* mine = lds + wave * kWave;
+  const int wat = lr * 128, wsw = lr / 2;
+  auto put = [&](int i, v4i x) {
+    const int at = i < A8 ? 8 * i : 16 * MT + 8 * (i - A8);  // first row of the load
+    *reinterpret_cast<v4i*>(mine + at * 128 + wat + ((lc ^ (at / 2 % 8 + wsw)) << 4)) = x;
+  };
   v4i acc[MT][NT] = {};
-  const int full = (int)(g.K / 128);
-  auto mma = [&](const v4i (&w)[NT][2], const v4i (&a)[MT][2]) {
+  auto mma = [&]() {
 #pragma unroll
-    for (int h = 0; h < 2; ++h)
+    for (int h = 0; h < 2; ++h) {
+      const int at = r * 128 + (((4 * h + q) ^ (r / 2)) << 4);
+      v4i a[MT], w[NT];
+#pragma unroll
+      for (int i = 0; i < MT; ++i) a[i] = *reinterpret_cast<const v4i*>(mine + i * 2048 + at);
+#pragma unroll
+      for (int j = 0; j < NT; ++j) w[j] = *reinterpret_cast<const v4i*>(mine + (MT + j) * 2048 + at);
 #pragma unroll
       for (int i = 0; i < MT; ++i)
 #pragma unroll
         for (int j = 0; j < NT; ++j)
-          acc[i][j] = __builtin_amdgcn_mfma_i32_16x16x64_i8(a[i][h], w[j][h], acc[i][j], 0, 0, 0);
+          acc[i][j] = __builtin_amdgcn_mfma_i32_16x16x64_i8(a[i], w[j], acc[i][j], 0, 0, 0);
+    }
   };
-  int sgm = wave;
-  for (; sgm + 8 * (U - 1) < full; sgm += 8 * U) {
-    v4i w[U][NT][2], a[U][MT][2];
+  auto order = [&]() { __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront", "local"); };
+  const int full = (int)(g.K / 128);
+  const int k0 = wave * 128 + 16 * lc;
+  v4i x[U][NL];
+#pragma unroll
+  for (int u = 0; u < U; ++u)
+    if (wave + 8 * u < full) {
+#pragma unroll
+      for (int i = 0; i < NL; ++i) x[u][i] = load16(row[i] + k0 + 1024 * u);
+    }
+  for (int sg = wave; sg < full; sg += 8 * U) {
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-      const int64_t k = (int64_t)(sgm + 8 * u) * 128;
+      if (sg + 8 * u < full) {
 #pragma unroll
-      for (int j = 0; j < NT; ++j) w[u][j][0] = load16(wr[j] + k), w[u][j][1] = load16(wr[j] + k + 64);
+        for (int i = 0; i < NL; ++i) put(i, x[u][i]);
+        if (sg + 8 * (u + U) < full) {
+          const int64_t k = (int64_t)(sg + 8 * (u + U)) * 128 + 16 * lc;
 #pragma unroll
-      for (int i = 0; i < MT; ++i) a[u][i][0] = load16(ar[i] + k), a[u][i][1] = load16(ar[i] + k + 64);
+          for (int i = 0; i < NL; ++i) x[u][i] = load16(row[i] + k);
+        }
+        order();
+        mma();
+        order();
+      }
     }
-#pragma unroll
-    for (int u = 0; u < U; ++u) mma(w[u], a[u]);
-  }
-  for (; sgm < full; sgm += 8) {
-    const int64_t k = (int64_t)sgm * 128;
-    v4i w[NT][2], a[MT][2];
-#pragma unroll
-    for (int j = 0; j < NT; ++j) w[j][0] = load16(wr[j] + k), w[j][1] = load16(wr[j] + k + 64);
-#pragma unroll
-    for (int i = 0; i < MT; ++i) a[i][0] = load16(ar[i] + k), a[i][1] = load16(ar[i] + k + 64);
-    mma(w, a);
   }
   if (g.K % 128 && wave == full % 8) {
-    const int64_t k = (int64_t)full * 128 + 16 * q;
-    v4i w[NT][2], a[MT][2];
 #pragma unroll
-    for (int h = 0; h < 2; ++h) {
-#pragma unroll
-      for (int j = 0; j < NT; ++j) w[j][h] = load16_to(wr[j] - 16 * q, k + 64 * h, g.K);
-#pragma unroll
-      for (int i = 0; i < MT; ++i) a[i][h] = load16_to(ar[i] - 16 * q, k + 64 * h, g.K);
-    }
-    mma(w, a);
+    for (int i = 0; i < NL; ++i) put(i, load16_to(row[i], (int64_t)full * 128 + 16 * lc, g.K));
+    order();
+    mma();
   }
+  __syncthreads();
+  int* red = reinterpret_cast<int*>(lds);  // [wave][tile][e][lane]
 #pragma unroll
   for (int i = 0; i < MT; ++i)
 #pragma unroll
     for (int j = 0; j < NT; ++j)
 #pragma unroll
-      for (int e = 0; e < 4; ++e) red[wave][i * NT + j][e][lane] = acc[i][j][e];
+      for (int e = 0; e < 4; ++e) red[((wave * MT * NT + i * NT + j) * 4 + e) * 64 + lane] = acc[i][j][e];
   __syncthreads();
-  for (int x = tid; x < MT * NT * 256; x += 512) {
-    const int tile = x / 256, e = x / 64 % 4, l = x % 64;
+  for (int y = tid; y < MT * NT * 256; y += 512) {
+    const int tile = y / 256, e = y / 64 % 4, l = y % 64;
     const int64_t m = 16 * (tile / NT) + 4 * (l / 16) + e, n = n0 + 16 * (tile % NT) + l % 16;
     if (m >= g.M || n >= g.N) continue;
     int sum = 0;
 #pragma unroll
-    for (int w = 0; w < 8; ++w) sum += red[w][tile][e][l];
-    float y = scaled(sum, g.sa[m], g.sw[n]);
-    if (g.bias) y = __fadd_rn(y, g.bias[n]);
-    store_y(g, m * g.ldy + n, y);
+    for (int w = 0; w < 8; ++w) sum += red[((w * MT * NT + tile) * 4 + e) * 64 + l];
+    float v = scaled(sum, g.sa[m], g.sw[n]);
+    if (g.bias) v = __fadd_rn(v, g.bias[n]);
+    store_y(g, m * g.ldy + n, v);
+  }
+}
+
+// One to four tokens with their quantization in the same launch: every
+// workgroup makes the codes for itself (at most kFusedMost elements, 32 a
+// thread), in LDS, while its first weights are on their way.  16 output
+// channels a workgroup, K over the waves as above.
+constexpr int kFusedMost = 16384;
+
+template <int TYPE>
+__global__ __launch_bounds__(512) void k_i8_fused(I8Gemm g, const typename Value<TYPE>::T* A, int64_t lda) {
+  constexpr int U = 4, kPad = 144, kHeld = kFusedMost / (8 * 512);
+  // codes of token m at m * (K up to a multiple of 128 + 16), then the waves'
+  // weights (later the sums), then the largest |x| and the scale of each token
+  __shared__ __align__(16) int8_t codes[kFusedMost + 4 * kPad];
+  __shared__ __align__(16) int8_t wlds[8 * 2048];
+  __shared__ uint32_t amax[4];
+  __shared__ float sa[4];
+  const int tid = threadIdx.x, lane = tid % 64, r = lane % 16, q = lane / 16;
+  const int wave = __builtin_amdgcn_readfirstlane(tid / 64);
+  const int M = (int)g.M, K = (int)g.K, nv = (K + 7) / 8, pitch = (K + 127) / 128 * 128 + 16;
+  const int64_t n0 = (int64_t)blockIdx.x * 16;
+  const int lr = lane / 8, lc = lane % 8;
+
+  Eight<TYPE> x[kHeld];
+  int xm[kHeld], xk[kHeld];
+#pragma unroll
+  for (int i = 0; i < kHeld; ++i) {
+    const int v = tid + 512 * i;
+    xm[i] = v / nv, xk[i] = v % nv * 8;
+    const bool on = xm[i] < M;
+    x[i].load(A + (on ? xm[i] : 0) * lda, on ? xk[i] : K, K);  // zeros past the last token
+  }
+  const int8_t* row[2];
+#pragma unroll
+  for (int i = 0; i < 2; ++i) row[i] = g.W + min(n0 + 8 * i + lr, g.N - 1) * g.ldw;
+  const int full = K / 128;
+  v4i w[U][2];
+#pragma unroll
+  for (int u = 0; u < U; ++u)
+    if (wave + 8 * u < full) {
+#pragma unroll
+      for (int i = 0; i < 2; ++i) w[u][i] = load16(row[i] + (wave + 8 * u) * 128 + 16 * lc);
+    }
+  if (tid < 4) amax[tid] = 0;
+  lds_barrier();
+#pragma unroll
+  for (int i = 0; i < kHeld; ++i) {
+    if (512 * i >= nv * M) break;
+    const uint32_t mx = x[i].amax();
+    if (nv % 64 == 0) {  // a wave's pieces are of one token
+      const uint32_t wm = wave_max(mx);
+      if (lane == 0 && xm[i] < M) atomicMax(&amax[xm[i]], wm);
+    } else if (xm[i] < M) {
+      atomicMax(&amax[xm[i]], mx);
+    }
+  }
+  lds_barrier();
+#pragma unroll
+  for (int i = 0; i < kHeld; ++i) {
+    if (xm[i] < M) {
+      const RowCoder rc(amax[xm[i]], 127.0f);
+      if (xk[i] == 0) sa[xm[i]] = rc.s;
+      *reinterpret_cast<uint2*>(codes + xm[i] * pitch + xk[i]) = x[i].codes(rc);
+    }
+  }
+  // the last segment's channels past K: zeros (products with whatever the weights hold there are 0 too)
+  for (int i = tid; i < 128 * M; i += 512) {
+    const int k = full * 128 + i % 128;
+    if (k >= nv * 8 && k < pitch) codes[i / 128 * pitch + k] = 0;
+  }
+  lds_barrier();
+
+  int8_t* mine = wlds + wave * 2048;
+  const int8_t* arow = codes + min(r, M - 1) * pitch + 16 * q;
+  v4i acc = {0, 0, 0, 0};
+  auto put = [&](int i, v4i v) {
+    *reinterpret_cast<v4i*>(mine + (8 * i + lr) * 128 + ((lc ^ (4 * i + lr / 2)) << 4)) = v;
+  };
+  auto mma = [&](int sg) {
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const v4i b = *reinterpret_cast<const v4i*>(mine + r * 128 + (((4 * h + q) ^ (r / 2)) << 4));
+      const v4i a = *reinterpret_cast<const v4i*>(arow + sg * 128 + 64 * h);
+      acc = __builtin_amdgcn_mfma_i32_16x16x64_i8(a, b, acc, 0, 0, 0);
+    }
+  };
+  auto order = [&]() { __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront", "local"); };
+  for (int sg = wave; sg < full; sg += 8 * U) {
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      if (sg + 8 * u < full) {
+#pragma unroll
+        for (int i = 0; i < 2; ++i) put(i, w[u][i]);
+        if (sg + 8 * (u + U) < full) {
+#pragma unroll
+          for (int i = 0; i < 2; ++i) w[u][i] = load16(row[i] + (sg + 8 * (u + U)) * 128 + 16 * lc);
+        }
+        order();
+        mma(sg + 8 * u);
+        order();
+      }
+    }
+  }
+  if (K % 128 && wave == full % 8) {
+#pragma unroll
+    for (int i = 0; i < 2; ++i) put(i, load16_to(row[i], (int64_t)full * 128 + 16 * lc, K));
+    order();
+    mma(full);
+  }
+  __syncthreads();
+  int* red = reinterpret_cast<int*>(wlds);  // [wave][e][column]: tokens 0 .. 3 are in the first 16 lanes
+  if (q == 0) {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) red[(wave * 4 + e) * 16 + r] = acc[e];
+  }
+  __syncthreads();
+  const int64_t n = n0 + tid % 16;
+  if (tid < 16 * M && n < g.N) {
+    const int m = tid / 16;
+    int sum = 0;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) sum += red[(i * 4 + m) * 16 + tid % 16];
+    float v = scaled(sum, sa[m], g.sw[n]);
+    if (g.bias) v = __fadd_rn(v, g.bias[n]);
+    store_y(g, m * g.ldy + n, v);
   }
 }
 
@@ -540,12 +688,23 @@ void launch_tile(const I8Gemm& g, hipStream_t stream) {
   k_i8_tile<BM, BN, CLAMP><<<(unsigned)((tm * tn + 7) / 8 * 8), 256, 0, stream>>>(g, (int)tm, (int)tn);
 }
 
-template <int MT>
+// Up to 16 tokens and 8192 channels, a workgroup takes 16 channels: the
+// weights are all that counts, and more workgroups load them sooner.  Else 48:
+// the tokens' codes are read once a workgroup, from L2, and would outweigh the
+// weights (40 x 11008 x 4096: 12.8 us a call with 16 channels, 11.9 with 48;
+// 64 tokens: 18.8 and 13.0; 48 x 4096 x 4096: 7.1 and 8.7).
+template <int A8>
 void launch_skinny(const I8Gemm& g, hipStream_t stream) {
-  if (MT <= 2 || g.N <= 4096)
-    k_i8_skinny<MT, 1><<<(unsigned)((g.N + 15) / 16), 512, 0, stream>>>(g);
+  if (A8 <= 2 || g.N <= 8192)
+    k_i8_skinny<A8, 1><<<(unsigned)((g.N + 15) / 16), 512, 0, stream>>>(g);
   else
-    k_i8_skinny<MT, 2><<<(unsigned)((g.N + 31) / 32), 512, 0, stream>>>(g);
+    k_i8_skinny<A8, 3><<<(unsigned)((g.N + 47) / 48), 512, 0, stream>>>(g);
+}
+
+template <int TYPE>
+void launch_fused(const I8Gemm& g, const void* A, int64_t lda, hipStream_t stream) {
+  const auto* a = static_cast<const typename Value<TYPE>::T*>(A);
+  k_i8_fused<TYPE><<<(unsigned)((g.N + 15) / 16), 512, 0, stream>>>(g, a, lda);
 }
 
 }  // namespace
@@ -558,11 +717,21 @@ hipError_t launch_quantize_rows(const void* A, int a_type, int64_t M, int64_t K,
   return hipGetLastError();
 }
 
+bool i8_fused(int64_t M, int64_t K) { return M <= 4 && M * ((K + 7) / 8 * 8) <= kFusedMost; }
+
+hipError_t launch_i8_fused(const I8Gemm& g, const void* A, int a_type, int64_t lda, hipStream_t stream) {
+  if (a_type == SONIQ_F32) launch_fused<SONIQ_F32>(g, A, lda, stream);
+  else if (a_type == SONIQ_BF16) launch_fused<SONIQ_BF16>(g, A, lda, stream);
+  else launch_fused<SONIQ_F16>(g, A, lda, stream);
+  return hipGetLastError();
+}
+
 hipError_t launch_i8_gemm(const I8Gemm& g, hipStream_t stream) {
-  if (g.M <= 16) launch_skinny<1>(g, stream);
-  else if (g.M <= 32) launch_skinny<2>(g, stream);
-  else if (g.M <= 48) launch_skinny<3>(g, stream);
-  else if (g.M <= 64) launch_skinny<4>(g, stream);
+  if (g.M <= 8) launch_skinny<1>(g, stream);
+  else if (g.M <= 16) launch_skinny<2>(g, stream);
+  else if (g.M <= 32) launch_skinny<4>(g, stream);
+  else if (g.M <= 48) launch_skinny<6>(g, stream);
+  else if (g.M <= 64) launch_skinny<8>(g, stream);
   else if (g.K < 16) k_i8_short<<<dim3((unsigned)((g.N + 255) / 256), (unsigned)std::min<int64_t>(g.M, 65535)), 256, 0, stream>>>(g);
   else if (std::max(g.lda, g.ldw) >= 1 << 24 || g.N < 64) launch_tile<64, 64, true>(g, stream);
   else if (((g.M + 255) / 256) * ((g.N + 255) / 256) >= 200 && std::min(g.M, g.N) >= 256) launch_tile<256, 256, false>(g, stream);

@@ -29,6 +29,10 @@ struct I8Gemm {
   int64_t ldy;
 };
 hipError_t launch_i8_gemm(const I8Gemm& g, hipStream_t stream);
+// Quantization and product in one launch, where they are (g.A and g.sa are
+// not read).
+bool i8_fused(int64_t M, int64_t K);
+hipError_t launch_i8_fused(const I8Gemm& g, const void* A, int a_type, int64_t lda, hipStream_t stream);
 
 // ---- key/value cache -------------------------------------------------------
 // One side of the cache and the ragged rows that go with it.

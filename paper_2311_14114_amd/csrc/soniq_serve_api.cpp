@@ -77,10 +77,14 @@ soniq_status check_gemm(const char* who, const void* W, int64_t ldw, const float
   return SONIQ_OK;
 }
 
-// Workspace of soniq_quantize_i8_gemm: the codes, rows of a multiple of 16
-// bytes, then the scales.
-int64_t codes_ld(int64_t K) { return round_up(K, 16); }
-int64_t i8_work(int64_t M, int64_t K) { return M * codes_ld(K) + round_up(4 * M, 16); }
+// Workspace of soniq_quantize_i8_gemm where it takes two launches: the codes,
+// then the scales.  Rows are padded past a multiple of 128 bytes, so that the
+// same chunk of neighbouring rows does not fall on one cache channel (8192^3:
+// 497 us on rows of 8192 bytes, 468 on 8320).
+int64_t codes_ld(int64_t K) { return round_up(K, 128) + 128; }
+int64_t i8_work(int64_t M, int64_t K) {
+  return i8_fused(M, K) ? 0 : M * codes_ld(K) + round_up(4 * M, 16);
+}
 
 soniq_status check_cache(const char* who, const soniq_kv_cache_t* c) {
   NEED(c, "%s: null cache", who);
@@ -203,9 +207,15 @@ soniq_status soniq_quantize_i8_gemm(const void* A_dev, int a_type, int64_t lda,
   if (soniq_status st = check_quantize(who, A_dev, a_type, M, K, lda)) return st;
   if (soniq_status st = check_gemm(who, W_dev, ldw, s_w_dev, bias_dev, M, N, K, Y_dev, y_type, ldy))
     return st;
-  NEED(work_bytes >= i8_work(M, K) && (work_dev || M == 0) && aligned(work_dev, 16),
-       "%s: a workspace of %lld bytes, 16-byte aligned, is needed", who, (long long)i8_work(M, K));
+  const int64_t need = i8_work(M, K);
+  NEED(work_bytes >= need && (work_dev || need == 0) && aligned(work_dev, 16),
+       "%s: a workspace of %lld bytes, 16-byte aligned, is needed", who, (long long)need);
   if (M == 0) return SONIQ_OK;
+  if (i8_fused(M, K)) {
+    const I8Gemm g{nullptr, 0, nullptr, W_dev, ldw, s_w_dev, bias_dev, M, N, K, Y_dev, y_type, ldy};
+    HIP_TRY(launch_i8_fused(g, A_dev, a_type, lda, hip_stream(stream)));
+    return SONIQ_OK;
+  }
   int8_t* q = static_cast<int8_t*>(work_dev);
   float* s = reinterpret_cast<float*>(q + M * codes_ld(K));
   const I8Gemm g{q, codes_ld(K), s, W_dev, ldw, s_w_dev, bias_dev, M, N, K, Y_dev, y_type, ldy};

@@ -34,7 +34,12 @@ template <>
 struct Value<SONIQ_F16> {
   typedef _Float16 T;
   static __device__ __forceinline__ float load(T v) { return (float)v; }
-  static __device__ __forceinline__ T store(float x) { return (_Float16)x; }
+  static __device__ __forceinline__ T store(float x) {
+    // x is a rounded fp32 value: without this a product and its conversion
+    // become one instruction that rounds once, here and there
+    asm("" : "+v"(x));
+    return (_Float16)x;
+  }
 };
 
 // The symmetric codec of a row whose largest |x| has the bits `amax` (as an

@@ -115,7 +115,9 @@ def test_i8_gemm(M, N, K, form):
 
 @pytest.mark.parametrize("M,N,K,gap", [(1, 4096, 4096, 0), (1, 33, 100, 3), (2, 1100, 768, 0), (3, 100, 8191, 1),
                                        (4, 256, 2048, 0), (5, 64, 512, 0), (8, 130, 11008, 0), (9, 40, 65, 0),
-                                       (40, 300, 1024, 5), (300, 512, 640, 0), (1, 24, 65536, 0)])
+                                       (40, 300, 1024, 5), (300, 512, 640, 0), (1, 24, 65536, 0),
+                                       (1, 100, 1, 0), (1, 70, 16384, 0), (1, 70, 16385, 1), (2, 40, 8192, 0), (2, 40, 513, 7),
+                                       (3, 129, 63, 0), (4, 16, 4089, 0), (4, 16, 4097, 0), (4, 5000, 127, 2), (55, 8200, 300, 0)])
 @pytest.mark.parametrize("dtype", ["fp32", "bf16", "fp16"])
 def test_quantize_i8_gemm_equals_the_two_calls(M, N, K, gap, dtype):
     A = _tokens(M, K, dtype, gap)
