@@ -657,7 +657,8 @@ soniq_status soniq_kv_read(const soniq_kv_cache_t* cache, void* K_dev, int64_t k
  *              B, max_q, max_kv; holds nothing between calls, and calls
  *              that may overlap need one each
  * T = 0 or B = 0 does nothing.  The same arguments give the same bits on
- * every call.  Errors: INVALID_ARGUMENT, UNSUPPORTED, HIP.
+ * every call.  Errors: INVALID_ARGUMENT, UNSUPPORTED (T * q_heads >= 2^24,
+ * B * heads * query rows / 16 >= 2^22, and the limits above), HIP.
  */
 soniq_status soniq_kv_attention(const soniq_kv_cache_t* cache, const void* q_dev,
                                 int64_t q_token_stride, int64_t q_head_stride, int type, int64_t T,

@@ -3,6 +3,7 @@
 #include "soniq_values.h"
 
 #include <algorithm>
+#include <type_traits>
 
 namespace soniq {
 namespace {
@@ -276,13 +277,11 @@ struct KvLds {
   int32_t qi[16 * R];            // per row: its query, -1 for none
 };
 
-__device__ __forceinline__ float q_value(const void* p, int64_t i, int type) {
-  return type == SONIQ_BF16 ? bf16_value(static_cast<const uint16_t*>(p)[i])
-                            : (float)static_cast<const _Float16*>(p)[i];
-}
+// Waves a SIMD, by the registers that a row tile's outputs take.
+constexpr int kv_waves(int D, int R) { return D * R <= 128 ? 4 : D == 128 ? 3 : 2; }
 
 template <int D, int BITS, int R>
-__global__ __launch_bounds__(256, 2) void k_kv_attend(KvAttend a, KvSplit sp) {
+__global__ __launch_bounds__(256, kv_waves(D, R)) void k_kv_attend(KvAttend a, KvSplit sp) {
   constexpr int RB = D * BITS / 8;   // bytes of a cache row
   constexpr int KB = RB / 4, VB = RB / 16;
   constexpr int NK = D / 32;         // products over d
@@ -313,56 +312,66 @@ __global__ __launch_bounds__(256, 2) void k_kv_attend(KvAttend a, KvSplit sp) {
   const int tid = threadIdx.x, lane = tid % 64, c = lane % 16, kb = lane / 16;
   const int wave = __builtin_amdgcn_readfirstlane(tid / 64);  // uniform, and known to be
 
-  // ---- queries: scaled to fp16, in operand order
-  {
-    // threads a row: a power of two that leaves each a multiple of 8 elements
-    constexpr int kMost = D % 128 == 0 ? 16 : 8, TPR = 16 / R < kMost ? 16 / R : kMost;
-    constexpr int PER = D / TPR;
-    if (tid < 16 * R * TPR) {
-      const int r = tid / TPR, d0 = tid % TPR * PER;
-      float x[PER];
-      uint32_t mx = 0;
-      if (r < rows) {
-        const int64_t t = span.first + (row0 + r) / G;
-        const int64_t at = t * a.q_ts + ((int64_t)h * G + (row0 + r) % G) * a.q_hs + d0;
+  // ---- the queries' loads go out before anything waits; they become operands
+  // while the first K and V are on their way
+  // threads a row: a power of two that leaves each a multiple of 8 elements
+  constexpr int kMost = D % 128 == 0 ? 16 : 8, TPR = 16 / R < kMost ? 16 / R : kMost;
+  constexpr int PER = D / TPR;
+  struct __attribute__((packed, aligned(2))) QP { uint16_t v[8]; };
+  QP qraw[PER / 8];
+  const int qr = tid / TPR, qd = tid % TPR * PER;
+  auto load_q = [&]() {
+    if (qr < rows) {  // rows <= 16 R: the threads past them have none
+      const int64_t t = span.first + (row0 + qr) / G;
+      const int64_t at = t * a.q_ts + ((int64_t)h * G + (row0 + qr) % G) * a.q_hs + qd;
+      const uint16_t* p = static_cast<const uint16_t*>(a.q) + at;
 #pragma unroll
-        for (int i = 0; i < PER; ++i) x[i] = q_value(a.q, at + i, a.type);
-      } else {
+      for (int g = 0; g < PER / 8; ++g) qraw[g] = *reinterpret_cast<const QP*>(p + 8 * g);
+    } else {
 #pragma unroll
-        for (int i = 0; i < PER; ++i) x[i] = 0.0f;
-      }
+      for (int g = 0; g < PER / 8; ++g)
 #pragma unroll
-      for (int i = 0; i < PER; ++i) mx = max(mx, __float_as_uint(x[i]) & 0x7FFFFFFFu);
-#pragma unroll
-      for (int o = 1; o < TPR; o *= 2) mx = max(mx, (uint32_t)__shfl_xor((int)mx, o));
-      // largest element to [2^14, 2^15); rows of zeros, infinities or NaN as they are
-      int e = (int)(mx >> 23) - 127 - 14;
-      e = mx >= 0x7F800000u || mx == 0 ? 0 : max(e, -100);
-      const float down = copysignf(__uint_as_float((uint32_t)(127 - e) << 23), a.scale);
-      float sum = 0.0f;
-#pragma unroll
-      for (int g = 0; g < PER / 8; ++g) {
-        h8 v;
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          const _Float16 y = (_Float16)(x[8 * g + i] * down);
-          v[k_order<BITS>(i)] = y;
-          sum += (float)y;
-        }
-        const int d = d0 + 8 * g;
-        L.q[r / 16][d % (D / 4) / 8][d / (D / 4) * 16 + r % 16] = v;
-      }
-#pragma unroll
-      for (int o = 1; o < TPR; o *= 2) sum += __shfl_xor(sum, o);
-      if (tid % TPR == 0) {
-        L.qf[r] = fabsf(a.scale) * 1.44269504f * 0x1p24f * __uint_as_float((uint32_t)(127 + e) << 23);
-        L.qz[r] = sum * (BITS == 8 ? -0x1p-17f : -0x1p-21f);
-        L.qi[r] = r < rows ? (row0 + r) / G : -1;
-      }
+        for (int i = 0; i < 8; ++i) qraw[g].v[i] = 0;
     }
-  }
+  };
+  auto stage_q = [&]() {
+    if (tid >= 16 * R * TPR) return;
+    float x[PER];
+    uint32_t mx = 0;
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+      const uint16_t u = qraw[i / 8].v[i % 8];
+      x[i] = a.type == SONIQ_BF16 ? bf16_value(u) : (float)__builtin_bit_cast(_Float16, u);
+      mx = max(mx, __float_as_uint(x[i]) & 0x7FFFFFFFu);
+    }
+#pragma unroll
+    for (int o = 1; o < TPR; o *= 2) mx = max(mx, (uint32_t)__shfl_xor((int)mx, o));
+    // largest element to [2^14, 2^15); rows of zeros, infinities or NaN as they are
+    int e = (int)(mx >> 23) - 127 - 14;
+    e = mx >= 0x7F800000u || mx == 0 ? 0 : max(e, -100);
+    const float down = copysignf(__uint_as_float((uint32_t)(127 - e) << 23), a.scale);
+    float sum = 0.0f;
+#pragma unroll
+    for (int g = 0; g < PER / 8; ++g) {
+      h8 v;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const _Float16 y = (_Float16)(x[8 * g + i] * down);
+        v[k_order<BITS>(i)] = y;
+        sum += (float)y;
+      }
+      const int d = qd + 8 * g;
+      L.q[qr / 16][d % (D / 4) / 8][d / (D / 4) * 16 + qr % 16] = v;
+    }
+#pragma unroll
+    for (int o = 1; o < TPR; o *= 2) sum += __shfl_xor(sum, o);
+    if (tid % TPR == 0) {
+      L.qf[qr] = fabsf(a.scale) * 1.44269504f * 0x1p24f * __uint_as_float((uint32_t)(127 + e) << 23);
+      L.qz[qr] = sum * (BITS == 8 ? -0x1p-17f : -0x1p-21f);
+      L.qi[qr] = qr < rows ? (row0 + qr) / G : -1;
+    }
+  };
 
-  // query of this lane's row in each tile (masked tiles ask)
   f4 O[R][DB];
   float m[R], l[R], sg[R], inv[R];
 #pragma unroll
@@ -391,16 +400,24 @@ __global__ __launch_bounds__(256, 2) void k_kv_attend(KvAttend a, KvSplit sp) {
     }
   };
 
-  for (int s0 = 0; s0 < pt.count; s0 += kSub) {
-    const int n = min(pt.count - s0, kSub), nst = (n + 31) / 32, p0 = pt.first + s0;
-    if (s0) lds_barrier();  // the last sub-part's rows and scales have been read
+  // Cache rows, validity and scales of positions [s0, s0 + kSub) of the part
+  // into LDS, with this wave's first K and V on their way.
+  auto prepare = [&](int s0, auto first) {
+    const int n = min(pt.count - s0, kSub), p0 = pt.first + s0;
     float kreg[kSub / 256], vreg[kSub / 256];
+    int32_t at[kSub / 256];
+#pragma unroll
+    for (int k = 0; k < kSub / 256; ++k) {
+      const int x = tid + 256 * k;
+      at[k] = x < n ? kv_row(a.table, a.dims, b, (int64_t)p0 + x) : -1;
+    }
+    if constexpr (decltype(first)::value) load_q();
 #pragma unroll
     for (int k = 0; k < kSub / 256; ++k) {
       const int x = tid + 256 * k;
       kreg[k] = vreg[k] = 0.0f;
       if (256 * k < n) {
-        int32_t row = x < n ? kv_row(a.table, a.dims, b, p0 + x) : -1;
+        int32_t row = at[k];
         const uint64_t there = __ballot(row >= 0);
         if (lane == 0) L.valid[x / 32] = (uint32_t)there;
         if (lane == 32) L.valid[x / 32] = (uint32_t)(there >> 32);
@@ -410,15 +427,20 @@ __global__ __launch_bounds__(256, 2) void k_kv_attend(KvAttend a, KvSplit sp) {
       }
     }
     lds_barrier();
-    if (wave < nst) {
+    if (wave < (n + 31) / 32) {
       load_k(wave);
       load_v(wave);
     }
+    if constexpr (decltype(first)::value) stage_q();
 #pragma unroll
     for (int k = 0; k < kSub / 256; ++k)
       if (256 * k < n) L.ks[tid + 256 * k] = kreg[k], L.vs[tid + 256 * k] = vreg[k];
     lds_barrier();
+  };
 
+  prepare(0, std::true_type());
+  for (int s0 = 0;;) {
+    const int n = min(pt.count - s0, kSub), nst = (n + 31) / 32, p0 = pt.first + s0;
     for (int st = wave; st < nst; st += 4) {
       const bool more = st + 4 < nst;
       f4 S[R][2];
@@ -535,13 +557,17 @@ __global__ __launch_bounds__(256, 2) void k_kv_attend(KvAttend a, KvSplit sp) {
       }
       if (more) load_v(st + 4);
     }
+    s0 += kSub;
+    if (s0 >= pt.count) break;
+    lds_barrier();  // this sub-part's rows and scales have been read
+    prepare(s0, std::false_type());
   }
 
   // ---- the four waves meet, one row tile at a time
   float* out = reinterpret_cast<float*>(lds_bytes);       // [wave][16][OP]
   float* ml = out + 4 * 16 * OP;                          // [wave][16][2]
   const bool direct = pt.used <= 1;
-  const int64_t stride = (int64_t)D + 2;
+  float* ml_out = a.work + (int64_t)a.T * a.q_heads * sp.parts * D;
 #pragma unroll
   for (int rt = 0; rt < R; ++rt) {
     __syncthreads();
@@ -586,45 +612,47 @@ __global__ __launch_bounds__(256, 2) void k_kv_attend(KvAttend a, KvSplit sp) {
         if (d == 0 && a.lse)
           a.lse[t * a.q_heads + hq] = sum == 0.0f ? -INFINITY : (M + __log2f(sum)) * 0.693147181f;
       } else {
-        float* w = a.work + ((t * a.q_heads + hq) * sp.parts + part) * stride;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) w[2 + d + i] = o[i];
-        if (d == 0) w[0] = M, w[1] = sum;
+        const int64_t x = (t * a.q_heads + hq) * sp.parts + part;
+        *reinterpret_cast<f4*>(a.work + x * D + d) = o;
+        if (d == 0) ml_out[2 * x] = M, ml_out[2 * x + 1] = sum;
       }
     }
   }
 }
 
-// One workgroup per (token, query head) joins its sequence's parts: wave w
-// takes parts w, w + 4, ..., then the four meet.
-template <int D>
+// Joins the parts of one (token, query head): W waves take every W-th part
+// each and meet in LDS (W = 1: a wave by itself, four rows a workgroup).
+template <int D, int W>
 __global__ __launch_bounds__(256) void k_kv_join(KvAttend a, KvSplit sp) {
-  constexpr int E = D / 64;
-  __shared__ float out[4][D], ml[4][2];
-  const int hq = blockIdx.y, tid = threadIdx.x, lane = tid % 64, wave = tid / 64;
-  const int64_t t = blockIdx.x;
+  constexpr int E = D / 64, kAhead = 4;
+  __shared__ float out[W == 1 ? 1 : W][D], ml[W == 1 ? 1 : W][2];
+  const int lane = threadIdx.x % 64, wave = threadIdx.x / 64;
+  const int64_t x = (int64_t)blockIdx.x * (4 / W) + (W == 1 ? wave : 0);
+  const int64_t t = x / a.q_heads;
+  const int hq = (int)(x % a.q_heads), first = W == 1 ? 0 : wave;
+  if (t >= a.T) return;
   const int b = row_sequence(a.cu, a.table.B, (int)t);
   if (b >= a.table.B) return;
   const KvSpan span = kv_span(a.cu[b], a.cu[b + 1], a.T);
   if (t < span.first || t - span.first >= min(span.count, a.max_q)) return;
   const KvPart pt = part_of(kv_length(a.table, a.dims, a.kv_len[b]), 0, sp.parts, sp.chunk);
   if (pt.used <= 1) return;  // written where it was computed
-  const int64_t stride = (int64_t)D + 2;
-  const float* w = a.work + (t * a.q_heads + hq) * sp.parts * stride;
+  const float* w = a.work + x * sp.parts * D;
+  const float* wml = a.work + (int64_t)a.T * a.q_heads * sp.parts * D + x * sp.parts * 2;
   float m = -INFINITY, l = 0.0f, o[E] = {};
-  // four parts' loads at a time (past the last one: its own again, weightless)
-  for (int p0 = wave; p0 < pt.used; p0 += 16) {
-    float pm[4], pl[4], po[4][E];
+  // kAhead parts' loads at a time (past the last one: the first again, weightless)
+  for (int p0 = first; p0 < pt.used; p0 += W * kAhead) {
+    float pm[kAhead], pl[kAhead], po[kAhead][E];
 #pragma unroll
-    for (int k = 0; k < 4; ++k) {
-      const bool on = p0 + 4 * k < pt.used;
-      const float* x = w + (on ? p0 + 4 * k : p0) * stride;
-      pm[k] = on ? x[0] : -INFINITY, pl[k] = on ? x[1] : 0.0f;
+    for (int k = 0; k < kAhead; ++k) {
+      const bool on = p0 + W * k < pt.used;
+      const int p = on ? p0 + W * k : p0;
+      pm[k] = on ? wml[2 * p] : -INFINITY, pl[k] = on ? wml[2 * p + 1] : 0.0f;
 #pragma unroll
-      for (int i = 0; i < E; ++i) po[k][i] = on ? x[2 + lane + 64 * i] : 0.0f;
+      for (int i = 0; i < E; ++i) po[k][i] = on ? w[(int64_t)p * D + E * lane + i] : 0.0f;
     }
 #pragma unroll
-    for (int k = 0; k < 4; ++k) {
+    for (int k = 0; k < kAhead; ++k) {
       const float mn = fmaxf(m, pm[k]), mu = mn == -INFINITY ? 0.0f : mn;
       const float al = __builtin_amdgcn_exp2f(m - mu), be = __builtin_amdgcn_exp2f(pm[k] - mu);
       l = l * al + pl[k] * be;  // a part that met a NaN alone has no maximum, but its sum
@@ -633,29 +661,36 @@ __global__ __launch_bounds__(256) void k_kv_join(KvAttend a, KvSplit sp) {
       m = mn;
     }
   }
+  if constexpr (W > 1) {
 #pragma unroll
-  for (int i = 0; i < E; ++i) out[wave][lane + 64 * i] = o[i];
-  if (lane == 0) ml[wave][0] = m, ml[wave][1] = l;
-  __syncthreads();
-  float M = fmaxf(fmaxf(ml[0][0], ml[1][0]), fmaxf(ml[2][0], ml[3][0]));
-  const float mu = M == -INFINITY ? 0.0f : M;
-  float f[4], sum = 0.0f;
+    for (int i = 0; i < E; ++i) out[wave][E * lane + i] = o[i];
+    if (lane == 0) ml[wave][0] = m, ml[wave][1] = l;
+    __syncthreads();
+    if (wave) return;
+    float M = -INFINITY;
 #pragma unroll
-  for (int x = 0; x < 4; ++x) {
-    f[x] = __builtin_amdgcn_exp2f(ml[x][0] - mu);
-    sum += ml[x][1] * f[x];
+    for (int k = 0; k < W; ++k) M = fmaxf(M, ml[k][0]);
+    const float mu = M == -INFINITY ? 0.0f : M;
+    l = 0.0f;
+#pragma unroll
+    for (int i = 0; i < E; ++i) o[i] = 0.0f;
+#pragma unroll
+    for (int k = 0; k < W; ++k) {
+      const float f = __builtin_amdgcn_exp2f(ml[k][0] - mu);
+      l += ml[k][1] * f;
+#pragma unroll
+      for (int i = 0; i < E; ++i) o[i] += out[k][E * lane + i] * f;
+    }
+    m = M;
   }
-  const float by = sum == 0.0f ? 0.0f : 1.0f / sum;
-  for (int d = tid; d < D; d += 256) {
-    float y = 0.0f;
+  const float by = l == 0.0f ? 0.0f : 1.0f / l;
+  const int64_t at = t * a.o_ts + hq * a.o_hs + E * lane;
 #pragma unroll
-    for (int x = 0; x < 4; ++x) y += out[x][d] * f[x];
-    y *= by;
-    const int64_t at = t * a.o_ts + hq * a.o_hs + d;
-    if (a.type == SONIQ_BF16) static_cast<uint16_t*>(a.out)[at] = bf16_bits(y);
-    else static_cast<_Float16*>(a.out)[at] = (_Float16)y;
+  for (int i = 0; i < E; ++i) {
+    if (a.type == SONIQ_BF16) static_cast<uint16_t*>(a.out)[at + i] = bf16_bits(o[i] * by);
+    else static_cast<_Float16*>(a.out)[at + i] = (_Float16)(o[i] * by);
   }
-  if (tid == 0 && a.lse) a.lse[t * a.q_heads + hq] = sum == 0.0f ? -INFINITY : (M + __log2f(sum)) * 0.693147181f;
+  if (lane == 0 && a.lse) a.lse[x] = l == 0.0f ? -INFINITY : (m + __log2f(l)) * 0.693147181f;
 }
 
 // Rows a workgroup takes, and how the positions are cut.  At least about a
@@ -686,7 +721,10 @@ void launch_attend(const KvAttend& a, const KvSplit& s, hipStream_t stream) {
   if (s.R == 1) k_kv_attend<D, BITS, 1><<<grid, block, 0, stream>>>(a, s);
   else if (s.R == 2) k_kv_attend<D, BITS, 2><<<grid, block, 0, stream>>>(a, s);
   else if constexpr (D <= 64) k_kv_attend<D, BITS, 4><<<grid, block, 0, stream>>>(a, s);
-  if (s.parts > 1) k_kv_join<D><<<dim3((unsigned)a.T, (unsigned)a.q_heads), 256, 0, stream>>>(a, s);
+  if (s.parts <= 1) return;
+  const int64_t x = (int64_t)a.T * a.q_heads;
+  if (s.parts <= 8) k_kv_join<D, 1><<<(unsigned)((x + 3) / 4), 256, 0, stream>>>(a, s);
+  else k_kv_join<D, 4><<<(unsigned)x, 256, 0, stream>>>(a, s);
 }
 
 template <bool WRITE, int D, int BITS>

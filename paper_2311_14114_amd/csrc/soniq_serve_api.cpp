@@ -149,8 +149,8 @@ soniq_status check_attend(const char* who, const soniq_kv_cache_t* cache, int64_
        q_heads, cache->heads);
   NEED(T >= 0 && B >= 0 && max_q >= 1 && max_kv >= 0, "%s: T = %lld, B = %lld, max_q = %lld, max_kv = %lld",
        who, (long long)T, (long long)B, (long long)max_q, (long long)max_kv);
-  LIMIT(max_q <= 256 && q_heads <= 65535 && B <= 65535 && max_kv < kMax31 && T < kMaxGroups,
-        "%s: max_q = %lld, %d query heads, B = %lld, T = %lld (max_q <= 256, heads and B < 2^16, T < 2^24)",
+  LIMIT(max_q <= 256 && q_heads <= 65535 && B <= 65535 && max_kv < kMax31 && T * q_heads < kMaxGroups,
+        "%s: max_q = %lld, %d query heads, B = %lld, T = %lld (max_q <= 256, heads and B < 2^16, T * heads < 2^24)",
         who, (long long)max_q, q_heads, (long long)B, (long long)T);
   LIMIT(B * cache->heads * ((max_q * (q_heads / cache->heads) + 15) / 16) < (1 << 22),
         "%s: %lld sequences of %d heads and up to %lld new tokens are too many", who, (long long)B,
