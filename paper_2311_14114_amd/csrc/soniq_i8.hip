@@ -57,42 +57,6 @@ __device__ __forceinline__ void lds_barrier() {
 }
 
 // ------------------------------------------------------------ quantizing --
-// Eight elements of a row, as loaded; elements from K on are zeros.
-template <int TYPE>
-struct Eight {
-  typename Value<TYPE>::T v[8];
-  __device__ __forceinline__ void load(const typename Value<TYPE>::T* row, int k, int K) {
-    if (k + 8 <= K) {
-      struct __attribute__((packed, aligned(sizeof(typename Value<TYPE>::T)))) P {
-        typename Value<TYPE>::T v[8];
-      };
-      __builtin_memcpy(v, reinterpret_cast<const P*>(row + k), sizeof v);
-    } else {
-#pragma unroll
-      for (int i = 0; i < 8; ++i) v[i] = k + i < K ? row[k + i] : (typename Value<TYPE>::T)0;
-    }
-  }
-  __device__ __forceinline__ uint32_t amax() const {
-    uint32_t m = 0;
-#pragma unroll
-    for (int i = 0; i < 8; ++i) m = max(m, __float_as_uint(Value<TYPE>::load(v[i])) & 0x7FFFFFFFu);
-    return m;
-  }
-  __device__ __forceinline__ uint2 codes(const RowCoder& c) const {
-    float x[8];
-#pragma unroll
-    for (int i = 0; i < 8; ++i) x[i] = Value<TYPE>::load(v[i]);
-    int q[8];
-    c.code<8>(x, q);
-    uint32_t w[2];
-#pragma unroll
-    for (int i = 0; i < 2; ++i)
-      w[i] = (uint32_t)(q[4 * i] & 255) | (uint32_t)(q[4 * i + 1] & 255) << 8 |
-             (uint32_t)(q[4 * i + 2] & 255) << 16 | (uint32_t)q[4 * i + 3] << 24;
-    return make_uint2(w[0], w[1]);
-  }
-};
-
 __device__ __forceinline__ void store_codes(int8_t* q, int k, int K, uint2 c) {
   if (k + 8 <= K) {
     struct __attribute__((packed, aligned(1))) P { uint2 v; };

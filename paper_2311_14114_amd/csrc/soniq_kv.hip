@@ -17,81 +17,124 @@ __device__ __forceinline__ int row_sequence(const int32_t* cu, int B, int t) {
   return b;
 }
 
-// A row of D elements is D / 8 lanes' work, 16 lanes for 64 elements too (8
-// of them idle), so that every row starts at a lane that 16 divides.  A wave
-// takes 64 / L rows: those of one token, heads of both sides in order.
+// Barrier for LDS alone: loads from memory stay in flight.
+__device__ __forceinline__ void lds_barrier() {
+  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup", "local");
+  __builtin_amdgcn_s_barrier();
+  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
+}
+
+// Rows of 8 codes a lane: 8, 16 or 32 lanes (24 of them busy for 192
+// elements) a row, so that a row's maximum stays within a wave.
 template <int D>
-constexpr int kRowLanes = D <= 128 ? 16 : 32;
+constexpr int kRowLanes = D == 64 ? 8 : D == 128 ? 16 : 32;
+constexpr int kCopyTokens = 16;  // tokens a workgroup, at most
 
+// A workgroup takes `tw` tokens, all heads of both sides.  Its first wave
+// finds where each token lives; then every thread moves pieces of 8 elements,
+// kAhead of them in flight (one at a time reached 3.7 TB/s on long reads:
+// 8 bytes a lane and 32 waves do not cover the memory's latency).
 template <int TYPE, int D, int BITS, bool WRITE>
-__global__ __launch_bounds__(256) void k_kv_copy(KvCopy c) {
+__global__ __launch_bounds__(256) void k_kv_copy(KvCopy c, int tw) {
   typedef typename Value<TYPE>::T T;
-  constexpr int L = kRowLanes<D>, PER = 64 / L, CB = BITS;  // CB: bytes of 8 codes
-  const int lane = threadIdx.x % 64, sub = lane / L, d = lane % L * 8;
-  const int H = c.dims.heads;
-  const int t = (int)blockIdx.x;
-  const int y = ((int)blockIdx.y * 4 + (int)threadIdx.x / 64) * PER + sub;  // row of the token
-  if (y - sub >= 2 * H) return;
-  const bool row_on = y < 2 * H, on = row_on && d < D;
-  const int h = y >= H ? y - H : y;
-  const bool second = y >= H;
-  const int64_t at = second ? (int64_t)t * c.side[1].token_stride + (int64_t)h * c.side[1].head_stride
-                            : (int64_t)t * c.side[0].token_stride + (int64_t)h * c.side[0].head_stride;
-  T* x = static_cast<T*>(second ? c.side[1].rows : c.side[0].rows) + at + d;
+  constexpr int L = kRowLanes<D>, kAhead = 4;
   struct __attribute__((packed, aligned(sizeof(T)))) P { T v[8]; };
-  P v;
-  if (WRITE && on) v = *reinterpret_cast<const P*>(x);
+  __shared__ int32_t where[kCopyTokens];  // row for head 0, -1 without a page, -2 behind the last sequence
+  const int tid = threadIdx.x, t0 = (int)blockIdx.x * tw, H2 = 2 * c.dims.heads;
+  const int tokens = min(tw, c.T - t0), pieces = tokens * H2 * L;
+  const int d = tid % L * 8;  // 256 is a multiple of L: the same elements of every row
+  const bool on = d < D;
 
-  const int b = row_sequence(c.cu, c.table.B, t);
-  if (b >= c.table.B) return;
-  const int32_t row0 = kv_row(c.table, c.dims, b, (int64_t)c.start[b] + ((int64_t)t - c.cu[b]));
-  const int64_t row = (int64_t)row0 + (int64_t)h * c.dims.page_size;
-  uint8_t* codes = (second ? c.side[1].codes : c.side[0].codes) + row * (D * BITS / 8) + d * BITS / 8;
-  float* scale = (second ? c.side[1].scale : c.side[0].scale) + row;
-  if (WRITE) {
-    if (row0 < 0) return;
-    float f[8];
-    uint32_t mx = 0;
+  Eight<TYPE> v[kAhead];
+  int64_t at[kAhead];    // element of the side's rows
+  int side[kAhead], head[kAhead], tok[kAhead];
+  auto place = [&](int k, int x) {
+    const int row = x / L;
+    tok[k] = row / H2;
+    const int y = row - tok[k] * H2;
+    side[k] = y >= c.dims.heads;
+    head[k] = side[k] ? y - c.dims.heads : y;
+    const int64_t t = t0 + tok[k];
+    at[k] = side[k] ? t * c.side[1].token_stride + head[k] * c.side[1].head_stride
+                    : t * c.side[0].token_stride + head[k] * c.side[0].head_stride;
+  };
+  auto rows = [&](int k) { return static_cast<T*>(side[k] ? c.side[1].rows : c.side[0].rows) + at[k] + d; };
+  auto load_rows = [&](int x0) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      f[i] = on ? Value<TYPE>::load(v.v[i]) : 0.0f;
-      mx = max(mx, __float_as_uint(f[i]) & 0x7FFFFFFFu);
+    for (int k = 0; k < kAhead; ++k)
+      if (x0 + 256 * k < pieces) {
+        place(k, x0 + 256 * k);
+        if (WRITE && on) v[k].load(rows(k));
+      }
+  };
+  load_rows(tid);
+
+  if (tid < 64) {
+    int b = 0;  // how many of cu[1 .. B] are at most this lane's token
+    for (int i = 0; i < c.table.B; i += 64) {
+      const int32_t end = i + tid < c.table.B ? c.cu[i + tid + 1] : 0;
+      const uint64_t live = __ballot(i + tid < c.table.B);
+#pragma unroll
+      for (int k = 0; k < kCopyTokens; ++k) {
+        const int n = __popcll(__ballot(end <= t0 + k) & live);
+        b += tid == k ? n : 0;
+      }
+    }
+    if (tid < tokens) {
+      int32_t row = -2;
+      if (b < c.table.B) row = kv_row(c.table, c.dims, b, (int64_t)c.start[b] + ((int64_t)(t0 + tid) - c.cu[b]));
+      where[tid] = row;
+    }
+  }
+  lds_barrier();
+
+  for (int x0 = tid; x0 < pieces;) {
+    int32_t row0[kAhead];
+    uint32_t w[kAhead][2];
+    float sc[kAhead];
+#pragma unroll
+    for (int k = 0; k < kAhead; ++k) {
+      row0[k] = x0 + 256 * k < pieces ? where[tok[k]] : -2;
+      w[k][0] = w[k][1] = 0;
+      sc[k] = 0.0f;
+      if (!WRITE && row0[k] >= 0 && on) {
+        const int64_t row = (int64_t)row0[k] + (int64_t)head[k] * c.dims.page_size;
+        const uint8_t* codes = (side[k] ? c.side[1].codes : c.side[0].codes) + row * (D * BITS / 8) + d * BITS / 8;
+        sc[k] = (side[k] ? c.side[1].scale : c.side[0].scale)[row];
+        if constexpr (BITS == 8) {
+          const uint2 x = *reinterpret_cast<const uint2*>(codes);
+          w[k][0] = x.x, w[k][1] = x.y;
+        } else {
+          w[k][0] = *reinterpret_cast<const uint32_t*>(codes);
+        }
+      }
     }
 #pragma unroll
-    for (int o = 1; o < L; o *= 2) mx = max(mx, (uint32_t)__shfl_xor((int)mx, o));
-    const RowCoder rc(mx, BITS == 8 ? 127.0f : 7.0f);
-    if (row_on && d == 0) *scale = rc.s;
-    int q[8];
-    rc.code<8>(f, q);
-    if (!on) return;
-    if constexpr (BITS == 8) {
-      uint32_t w[2];
+    for (int k = 0; k < kAhead; ++k) {
+      if (WRITE) {
+        uint32_t mx = on && row0[k] >= 0 ? v[k].amax() : 0;
 #pragma unroll
-      for (int i = 0; i < 2; ++i)
-        w[i] = (uint32_t)(q[4 * i] & 255) | (uint32_t)(q[4 * i + 1] & 255) << 8 |
-               (uint32_t)(q[4 * i + 2] & 255) << 16 | (uint32_t)q[4 * i + 3] << 24;
-      *reinterpret_cast<uint2*>(codes) = make_uint2(w[0], w[1]);
-    } else {
-      uint32_t w = 0;
+        for (int o = 1; o < L; o *= 2) mx = max(mx, (uint32_t)__shfl_xor((int)mx, o));
+        if (row0[k] < 0) continue;
+        const RowCoder rc(mx, BITS == 8 ? 127.0f : 7.0f);
+        const int64_t row = (int64_t)row0[k] + (int64_t)head[k] * c.dims.page_size;
+        if (d == 0) (side[k] ? c.side[1].scale : c.side[0].scale)[row] = rc.s;
+        if (!on) continue;
+        uint8_t* codes = (side[k] ? c.side[1].codes : c.side[0].codes) + row * (D * BITS / 8) + d * BITS / 8;
+        if constexpr (BITS == 8) *reinterpret_cast<uint2*>(codes) = v[k].codes(rc);
+        else *reinterpret_cast<uint32_t*>(codes) = v[k].nibbles(rc);
+      } else if (on && row0[k] > -2) {
+        P y;
 #pragma unroll
-      for (int i = 0; i < 8; ++i) w |= (uint32_t)(q[i] & 15) << (4 * i);
-      *reinterpret_cast<uint32_t*>(codes) = w;
+        for (int i = 0; i < 8; ++i) {
+          const int code = BITS == 8 ? (int8_t)(w[k][i / 4] >> (8 * (i % 4))) : (int)(w[k][0] << (28 - 4 * i)) >> 28;
+          y.v[i] = Value<TYPE>::store((float)code * sc[k]);
+        }
+        *reinterpret_cast<P*>(rows(k)) = y;
+      }
     }
-  } else {
-    if (!on) return;
-    uint32_t w[2] = {0, 0};
-    float s = 0.0f;
-    if (row0 >= 0) {
-      s = *scale;
-      w[0] = *reinterpret_cast<const uint32_t*>(codes);
-      if (BITS == 8) w[1] = *reinterpret_cast<const uint32_t*>(codes + 4);
-    }
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      const int code = BITS == 8 ? (int8_t)(w[i / 4] >> (8 * (i % 4))) : (int)(w[0] << (28 - 4 * i)) >> 28;
-      v.v[i] = Value<TYPE>::store((float)code * s);
-    }
-    *reinterpret_cast<P*>(x) = v;
+    x0 += 256 * kAhead;
+    load_rows(x0);
   }
 }
 
@@ -135,13 +178,6 @@ typedef float f4 __attribute__((ext_vector_type(4)));
 
 constexpr int kSub = 1024;     // positions whose rows and scales LDS holds at a time
 constexpr float kSgMin = 0x1p-120f;
-
-// Barrier for LDS alone: loads from memory stay in flight.
-__device__ __forceinline__ void lds_barrier() {
-  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup", "local");
-  __builtin_amdgcn_s_barrier();
-  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
-}
 
 // Over the four lanes that share c: the same result in each.
 __device__ __forceinline__ float quad_max(float x) {
@@ -729,11 +765,16 @@ void launch_attend(const KvAttend& a, const KvSplit& s, hipStream_t stream) {
 
 template <bool WRITE, int D, int BITS>
 void launch_kv_copy(const KvCopy& c, hipStream_t stream) {
-  constexpr int PER = 64 / kRowLanes<D>;
-  const dim3 grid((unsigned)c.T, (unsigned)((2 * c.dims.heads + 4 * PER - 1) / (4 * PER)));
-  if (c.type == SONIQ_F32) k_kv_copy<SONIQ_F32, D, BITS, WRITE><<<grid, 256, 0, stream>>>(c);
-  else if (c.type == SONIQ_BF16) k_kv_copy<SONIQ_BF16, D, BITS, WRITE><<<grid, 256, 0, stream>>>(c);
-  else k_kv_copy<SONIQ_F16, D, BITS, WRITE><<<grid, 256, 0, stream>>>(c);
+  // one token a workgroup until there are two thousand workgroups, then whole
+  // rounds of its pieces; writes take one round, whose codes cost arithmetic
+  // that other workgroups' loads hide
+  const int round = std::max(4 * 256 / (2 * c.dims.heads * kRowLanes<D>), 1);
+  int tw = std::min(std::max(c.T / 2048, 1), WRITE ? std::min(round, kCopyTokens) : kCopyTokens);
+  if (tw > round) tw = tw / round * round;
+  const unsigned grid = (unsigned)((c.T + tw - 1) / tw);
+  if (c.type == SONIQ_F32) k_kv_copy<SONIQ_F32, D, BITS, WRITE><<<grid, 256, 0, stream>>>(c, tw);
+  else if (c.type == SONIQ_BF16) k_kv_copy<SONIQ_BF16, D, BITS, WRITE><<<grid, 256, 0, stream>>>(c, tw);
+  else k_kv_copy<SONIQ_F16, D, BITS, WRITE><<<grid, 256, 0, stream>>>(c, tw);
 }
 template <bool WRITE>
 hipError_t launch_kv_copy(const KvCopy& c, hipStream_t stream) {

@@ -98,7 +98,7 @@ soniq_status check_cache(const char* who, const soniq_kv_cache_t* c) {
   LIMIT(c->head_dim == 64 || c->head_dim == 128 || c->head_dim == 192 || c->head_dim == 256,
         "%s: head_dim %d (64, 128, 192 and 256 are supported)", who, c->head_dim);
   LIMIT(c->bits == 4 || c->bits == 8, "%s: %d-bit cache (4 and 8 are supported)", who, c->bits);
-  LIMIT(c->heads <= 65535 && c->pages < kMax31 &&
+  LIMIT(c->heads < (1 << 14) && c->pages < kMax31 &&
             (int64_t)c->heads * c->page_size < kMax31 &&
             c->pages * ((int64_t)c->heads * c->page_size) < kMax31,
         "%s: %lld pages of %d rows for %d heads (2^31 rows or more)", who, (long long)c->pages,

@@ -48,11 +48,11 @@ struct Value<SONIQ_F16> {
 // infinity or NaN gives codes 0.
 //
 // The quotient comes from a reciprocal: v_rcp_f32 is good to one ulp, so for
-// |x / s| <= 128 the product is off by less than 2^-15, and rint of it is
-// rint of the true quotient's fp32 rounding unless it lies within 2^-14 of a
-// half-integer.  There, and for scales near the ends of fp32, the division
-// decides.  The clamp is for subnormal scales, whose own rounding can exceed
-// a step.
+// |x / s| <= 128 the product is off by less than 2^-15, and its nearest
+// integer is that of the true quotient's fp32 rounding unless it lies within
+// 2^-14 of a half-integer.  There, and for scales near the ends of fp32, the
+// division decides (the clamp is for subnormal scales, whose own rounding can
+// exceed a step).
 struct RowCoder {
   float s, rs, top;
   bool zero, fast;
@@ -62,21 +62,79 @@ struct RowCoder {
     fast = s >= 0x1p-100f && s <= 0x1p100f;
     rs = __builtin_amdgcn_rcpf(s);
   }
-  template <int N>
-  __device__ __forceinline__ void code(const float (&x)[N], int (&q)[N]) const {
-    float t[N], far = 0.0f;
+  // Four codes as the bytes of a word.  t = x / s + 1.5 * 2^23 holds the
+  // nearest integer in its low bits: no conversion, one byte permute a pair.
+  __device__ __forceinline__ uint32_t four(const float (&x)[4]) const {
+    if (zero) return 0;
+    constexpr float kMagic = 12582912.0f;
+    uint32_t t[4];
+    float far = 0.0f;
 #pragma unroll
-    for (int i = 0; i < N; ++i) {
-      const float e = x[i] * rs;
-      t[i] = __builtin_rintf(e);
-      far = fmaxf(far, fabsf(e - t[i]));  // at most a half
+    for (int i = 0; i < 4; ++i) {
+      const float y = __builtin_fmaf(x[i], rs, kMagic);
+      far = fmaxf(far, fabsf(__builtin_fmaf(x[i], rs, kMagic - y)));  // at most a half
+      t[i] = __float_as_uint(y);
     }
     if (!fast || far >= 0.5f - 0x1p-14f) {
 #pragma unroll
-      for (int i = 0; i < N; ++i) t[i] = fminf(fmaxf(__builtin_rintf(__fdiv_rn(x[i], s)), -top), top);
+      for (int i = 0; i < 4; ++i)
+        t[i] = (uint32_t)(int)fminf(fmaxf(__builtin_rintf(__fdiv_rn(x[i], s)), -top), top);
     }
+    const uint32_t lo = __builtin_amdgcn_perm(t[1], t[0], 0x0c0c0400u);
+    const uint32_t hi = __builtin_amdgcn_perm(t[3], t[2], 0x0c0c0400u);
+    return __builtin_amdgcn_perm(hi, lo, 0x05040100u);
+  }
+};
+
+// Eight neighbouring elements of a row, at any element's address.
+template <int TYPE>
+struct Eight {
+  typedef typename Value<TYPE>::T T;
+  T v[8];
+  // elements from K on are zeros, and not read
+  __device__ __forceinline__ void load(const T* row, int k, int K) {
+    if (k + 8 <= K) {
+      load(row + k);
+    } else {
 #pragma unroll
-    for (int i = 0; i < N; ++i) q[i] = zero ? 0 : (int)t[i];
+      for (int i = 0; i < 8; ++i) v[i] = k + i < K ? row[k + i] : (T)0;
+    }
+  }
+  __device__ __forceinline__ void load(const T* p) {
+    struct __attribute__((packed, aligned(sizeof(T)))) P { T v[8]; };
+    __builtin_memcpy(v, reinterpret_cast<const P*>(p), sizeof v);
+  }
+  // Bits of the largest |x| in fp32: their order as integers is that of the
+  // values, with NaN on top; 16-bit types compare two at a time.
+  __device__ __forceinline__ uint32_t amax() const {
+    if constexpr (TYPE == SONIQ_F32) {
+      uint32_t m = 0;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) m = max(m, __float_as_uint(v[i]) & 0x7FFFFFFFu);
+      return m;
+    } else {
+      typedef uint16_t u2 __attribute__((ext_vector_type(2)));
+      uint32_t w[4];
+      __builtin_memcpy(w, v, sizeof w);
+      u2 m = {0, 0};
+#pragma unroll
+      for (int i = 0; i < 4; ++i) m = __builtin_elementwise_max(m, __builtin_bit_cast(u2, w[i] & 0x7FFF7FFFu));
+      const uint16_t x = m[0] > m[1] ? m[0] : m[1];
+      return TYPE == SONIQ_BF16 ? (uint32_t)x << 16
+                                : __float_as_uint((float)__builtin_bit_cast(_Float16, x));
+    }
+  }
+  __device__ __forceinline__ uint2 codes(const RowCoder& c) const {
+    float x[2][4];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) x[i / 4][i % 4] = Value<TYPE>::load(v[i]);
+    return make_uint2(c.four(x[0]), c.four(x[1]));
+  }
+  // 4-bit codes, element 2i in the low half of byte i
+  __device__ __forceinline__ uint32_t nibbles(const RowCoder& c) const {
+    const uint2 w = codes(c);
+    const uint32_t a = w.x & 0x0F0F0F0Fu, b = w.y & 0x0F0F0F0Fu;
+    return __builtin_amdgcn_perm(b | b >> 4, a | a >> 4, 0x06040200u);
   }
 };
 
