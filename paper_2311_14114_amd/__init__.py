@@ -509,21 +509,23 @@ def soniq_act_wait_timeouts(act: Activations) -> int:
 # These calls take a few microseconds of GPU time at decode sizes, so their
 # checks are written to cost little: one query of the device and the stream a
 # call, sizes of workspaces remembered by their arguments.
+torch = None     # imported with the first call
 _TYPES = None
 
 
-def _types():
-    global _TYPES
+def _load():
+    global torch, _TYPES
     import torch
     _TYPES = {torch.float32: SONIQ_F32, torch.bfloat16: SONIQ_BF16, torch.float16: SONIQ_F16,
               torch.int8: None, torch.int32: None, torch.uint8: None, torch.int64: None}
-    return _TYPES
+    lib()
 
 
 def _device(t, what: str) -> int:
     """Index of the current device, where t has to be: the library works on the
     current device alone."""
-    import torch
+    if torch is None:
+        _load()
     if not isinstance(t, torch.Tensor) or not t.is_cuda:
         raise TypeError(f"{what} must be a device tensor")
     d = torch._C._cuda_getDevice()
@@ -535,12 +537,10 @@ def _device(t, what: str) -> int:
 def _raw_stream(stream, device: int):
     if stream is not None:
         return int(stream)
-    import torch
     return torch._C._cuda_getCurrentRawStream(device)
 
 
 def _refuse(t, what: str, d: int, dtype, dim: int):
-    import torch
     if not isinstance(t, torch.Tensor) or not t.is_cuda:
         raise TypeError(f"{what} must be a device tensor")
     if t.get_device() != d:
@@ -582,7 +582,7 @@ def _ld(t, what: str, M: int, K: int) -> int:
 
 
 def _type_of(t, what: str) -> int:
-    code = (_TYPES or _types()).get(t.dtype)
+    code = _TYPES.get(t.dtype)
     if code is None:
         raise TypeError(f"{what} must be float32, bfloat16 or float16")
     return code
@@ -592,7 +592,6 @@ def soniq_quantize_rows(A, out=None, scales=None, stream=None):
     """Symmetric 8-bit codes of the rows of A (device float32, bfloat16 or
     float16 [M, K]) with one scale each: tokens, or the output channels of a
     weight matrix.  Returns (codes int8 [M, K], scales float32 [M])."""
-    import torch
     d = _device(A, "A")
     ta = _type_of(A, "A")
     _is(A, "A", d, A.dtype, 2)
@@ -607,13 +606,12 @@ def soniq_quantize_rows(A, out=None, scales=None, stream=None):
     if scales is None:
         scales = torch.empty(M, dtype=torch.float32, device=A.device)
     s = _vector(scales, "scales", d, torch.float32, M)
-    _check(lib().soniq_quantize_rows(A.data_ptr(), ta, M, K, lda, out.data_ptr(), _ld(out, "out", M, K), s,
+    _check(_lib.soniq_quantize_rows(A.data_ptr(), ta, M, K, lda, out.data_ptr(), _ld(out, "out", M, K), s,
                                      _raw_stream(stream, d)))
     return out, scales
 
 
 def _i8_operands(W, s_w, bias, d, M, K, out, dtype, device):
-    import torch
     _is(W, "W", d, torch.int8, 2)
     N, Kw = W.shape
     if Kw != K:
@@ -632,13 +630,12 @@ def soniq_i8_gemm(A, s_a, W, s_w, bias=None, out=None, dtype=None, stream=None):
     """Y = (A W^T) * s_a[:, None] * s_w + bias of int8 codes A [M, K] and
     W [N, K] with float32 scales per row; Y [M, N] of `dtype` (bfloat16 unless
     given).  Returns Y."""
-    import torch
     d = _device(A, "A")
     _is(A, "A", d, torch.int8, 2)
     M, K = A.shape
     sa = _vector(s_a, "s_a", d, torch.float32, M)
     N, w, ldw, sw, b, out = _i8_operands(W, s_w, bias, d, M, K, out, dtype, A.device)
-    _check(lib().soniq_i8_gemm(A.data_ptr(), _ld(A, "A", M, K), sa, w, ldw, sw, b, M, N, K, out.data_ptr(),
+    _check(_lib.soniq_i8_gemm(A.data_ptr(), _ld(A, "A", M, K), sa, w, ldw, sw, b, M, N, K, out.data_ptr(),
                                _type_of(out, "out"), _ld(out, "out", M, N), _raw_stream(stream, d)))
     return out
 
@@ -651,7 +648,6 @@ def soniq_quantize_i8_gemm_workspace(M: int, K: int) -> int:
 
 
 def _work(work, need: int, d: int, device):
-    import torch
     if work is None:
         if need == 0:
             return None, 0, None
@@ -674,7 +670,7 @@ def soniq_quantize_i8_gemm(A, W, s_w, bias=None, out=None, dtype=None, work=None
     lda = _ld(A, "A", M, K)
     N, w, ldw, sw, b, out = _i8_operands(W, s_w, bias, d, M, K, out, dtype, A.device)
     wp, wn, work = _work(work, soniq_quantize_i8_gemm_workspace(M, K), d, A.device)
-    _check(lib().soniq_quantize_i8_gemm(A.data_ptr(), ta, lda, w, ldw, sw, b, M, N, K, out.data_ptr(),
+    _check(_lib.soniq_quantize_i8_gemm(A.data_ptr(), ta, lda, w, ldw, sw, b, M, N, K, out.data_ptr(),
                                         _type_of(out, "out"), _ld(out, "out", M, N), wp, wn,
                                         _raw_stream(stream, d)))
     return out
@@ -689,7 +685,6 @@ class KVCache:
     copy and move.  KVCache.empty makes them."""
 
     def __init__(self, k, k_scale, v, v_scale, bits: int = 8):
-        import torch
         d = _device(k, "k")
         for t, what in ((k, "k"), (v, "v")):
             _is(t, what, d, t.dtype, 4)
@@ -714,7 +709,8 @@ class KVCache:
     @classmethod
     def empty(cls, pages: int, page_size: int, heads: int, head_dim: int, bits: int = 8):
         """A cache of zeros on the current device."""
-        import torch
+        if torch is None:
+            _load()
         if bits not in (4, 8) or head_dim * bits % 8:
             raise ValueError("bits must be 4 or 8, and a row a whole number of bytes")
         device = torch.device("cuda", torch.cuda.current_device())
@@ -725,7 +721,6 @@ class KVCache:
 
 def _kv_batch(cache, page_table, cu, lengths, what):
     """Device, and (B, width, leading dimension, addresses) of a ragged batch."""
-    import torch
     d = cache.device_index
     if torch._C._cuda_getDevice() != d:
         raise ValueError(f"the cache is on {cache.device}, the current device is another one")
@@ -767,7 +762,7 @@ def soniq_kv_write(cache: KVCache, K, V, page_table, cu, start, stream=None) -> 
     T = K.shape[0]
     if tk != tv or T != V.shape[0]:
         raise ValueError("K and V must have one type and one number of tokens")
-    _check(lib().soniq_kv_write(cache._ref, K.data_ptr(), kts, khs, V.data_ptr(), vts, vhs, tk, T, table, ld, width,
+    _check(_lib.soniq_kv_write(cache._ref, K.data_ptr(), kts, khs, V.data_ptr(), vts, vhs, tk, T, table, ld, width,
                                 B, cu, start, _raw_stream(stream, d)))
 
 
@@ -776,7 +771,6 @@ def soniq_kv_read(cache: KVCache, page_table, cu, start, tokens: int, dtype=None
     row cu[b] + i of K and V [tokens, heads, head_dim] (of `dtype`, bfloat16
     unless given, or into the pair `out`).  Returns (K, V); rows from cu[B] on
     are left as they are (out=None: uninitialised)."""
-    import torch
     d, B, width, ld, table, cu, start = _kv_batch(cache, page_table, cu, start, "start")
     heads, D = cache.heads, cache.head_dim
     if out is None:
@@ -792,7 +786,7 @@ def soniq_kv_read(cache: KVCache, page_table, cu, start, tokens: int, dtype=None
             raise ValueError("K and V must have one type (dtype) and `tokens` rows")
         _kv_out(K, "K", kts, khs)
         _kv_out(V, "V", vts, vhs)
-    _check(lib().soniq_kv_read(cache._ref, K.data_ptr(), kts, khs, V.data_ptr(), vts, vhs, tk, tokens, table, ld,
+    _check(_lib.soniq_kv_read(cache._ref, K.data_ptr(), kts, khs, V.data_ptr(), vts, vhs, tk, tokens, table, ld,
                                width, B, cu, start, _raw_stream(stream, d)))
     return K, V
 
@@ -825,7 +819,6 @@ def soniq_kv_attention(cache: KVCache, q, page_table, cu, kv_len, scale=None, ma
     longest kv_len, a hint.  lse: a float32 [T, q_heads] tensor to fill.
     work: a uint8 device tensor of soniq_kv_attention_workspace(...) bytes
     (allocated when None).  Returns out (like q)."""
-    import torch
     d, B, width, ld, table, cu, kv_len = _kv_batch(cache, page_table, cu, kv_len, "kv_len")
     code = _type_of(q, "q")
     _is(q, "q", d, q.dtype, 3)
@@ -856,7 +849,7 @@ def soniq_kv_attention(cache: KVCache, q, page_table, cu, kv_len, scale=None, ma
     if max_kv is None:
         max_kv = width * cache.page_size
     wp, wn, work = _work(work, soniq_kv_attention_workspace(cache, T, heads, B, max_q, max_kv), d, cache.device)
-    _check(lib().soniq_kv_attention(cache._ref, q.data_ptr(), qts, qhs, code, T, heads, table, ld, width, B, cu,
+    _check(_lib.soniq_kv_attention(cache._ref, q.data_ptr(), qts, qhs, code, T, heads, table, ld, width, B, cu,
                                     kv_len, bits, words, D ** -0.5 if scale is None else scale, max_q, max_kv,
                                     out.data_ptr(), ots, ohs, None if lse is None else lse.data_ptr(), wp, wn,
                                     _raw_stream(stream, d)))

@@ -444,11 +444,16 @@ __device__ __forceinline__ void tile_out(const I8Gemm& g, const v16i (&acc)[TM][
 // neighbour computes the same outputs, to the same bits).  CLAMP: for
 // matrices smaller than a tile, and for row strides of 2^24 bytes and more:
 // each row's address by itself.
-template <int BM, int BN, bool CLAMP>
-__global__ __launch_bounds__(256, BM * BN > 128 * 128 ? 1 : 2) void k_i8_tile(I8Gemm g, int tm, int tn) {
+//
+// SETS = 2: two sets of four waves take the even and the odd stages, each
+// with its own buffers, and the first adds the second's sums before it stores.
+// Few tiles leave a CU with one workgroup, whose one stage in flight does not
+// cover the memory's latency.
+template <int BM, int BN, bool CLAMP, int SETS>
+__global__ __launch_bounds__(256 * SETS, BM * BN * SETS > 128 * 128 ? 1 : 2) void k_i8_tile(I8Gemm g, int tm, int tn) {
   constexpr int TM = BM / 64, TN = BN / 64;        // 32x32 tiles a wave
   constexpr int LA = BM / 32, LB = BN / 32, NS = LA + LB;  // 16-byte loads a thread and stage
-  __shared__ __align__(16) int8_t lds[2][(BM + BN) * 128];
+  __shared__ __align__(16) int8_t lds_all[SETS][2][(BM + BN) * 128];
 
   // Workgroup b runs on XCD b % 8: each XCD takes a contiguous run of the
   // tile order, columns of four row blocks, so that its L2 serves the rows
@@ -462,17 +467,22 @@ __global__ __launch_bounds__(256, BM * BN > 128 * 128 ? 1 : 2) void k_i8_tile(I8
     bm = 4 * band + in % rows;
     bn = in / rows;
   }
-  const int tid = threadIdx.x, lane = tid % 64;
+  const int set = SETS == 1 ? 0 : __builtin_amdgcn_readfirstlane(threadIdx.x / 256);
+  const int tid = threadIdx.x % 256, lane = tid % 64;
   const int wave = __builtin_amdgcn_readfirstlane(tid / 64);
+  auto& lds = lds_all[set];
   const int64_t m0 = CLAMP ? (int64_t)bm * BM : min((int64_t)bm * BM, g.M - BM);
   const int64_t n0 = CLAMP ? (int64_t)bn * BN : min((int64_t)bn * BN, g.N - BN);
   const int lr = tid / 8, lc = tid % 8;
-  const int stages = (int)((g.K + 127) / 128);
-  const bool tail = g.K % 128 != 0;
+  // Stages of this set (the second set's last one may lie past K altogether).
   // In a partial last stage, chunks that cross the end of a row are taken from
   // its last 16 bytes (K >= 16 here) and moved down when they are written;
   // `over`: how many bytes past the end this thread's chunk would reach.
-  const int over = max(0, 16 * lc + 16 - (int)(g.K - (int64_t)(stages - 1) * 128));
+  const int stages = ((int)((g.K + 127) / 128) + SETS - 1) / SETS;
+  const int left = (int)g.K - ((stages - 1) * SETS + set) * 128;  // of the last stage
+  const bool tail = left < 128;
+  const int over = max(0, 16 * lc + 16 - left);
+  constexpr uint32_t kStep = SETS * 128;
   const int8_t* row[NS];  // uniform without CLAMP
 #pragma unroll
   for (int i = 0; i < NS; ++i) {
@@ -483,7 +493,8 @@ __global__ __launch_bounds__(256, BM * BN > 128 * 128 ? 1 : 2) void k_i8_tile(I8
     else
       row[i] = isA ? g.A + (m0 + r) * g.lda : g.W + (n0 + r) * g.ldw;
   }
-  const uint32_t va = (CLAMP ? 0 : (uint32_t)(lr * g.lda)) + 16 * lc, vb = (CLAMP ? 0 : (uint32_t)(lr * g.ldw)) + 16 * lc;
+  const uint32_t va = (CLAMP ? 0 : (uint32_t)(lr * g.lda)) + 16 * lc + 128 * set;
+  const uint32_t vb = (CLAMP ? 0 : (uint32_t)(lr * g.ldw)) + 16 * lc + 128 * set;
   v4i st[NS];
   // k: byte of the rows where the stage starts (this thread's chunk is 16 lc further)
   auto load = [&](int i, uint32_t k) { st[i] = load16(row[i] + ((i < LA ? va : vb) + k)); };
@@ -557,14 +568,14 @@ __global__ __launch_bounds__(256, BM * BN > 128 * 128 ? 1 : 2) void k_i8_tile(I8
   for (int i = 0; i < NS; ++i) write(i, 0);
   if (stages > 1) {
 #pragma unroll
-    for (int i = 0; i < NS; ++i) load(i, 128u - (stages == 2 ? over : 0));
+    for (int i = 0; i < NS; ++i) load(i, kStep - (stages == 2 ? over : 0));
   }
   lds_barrier();
   read(f[0], 0, 0);
   int s = 0;
   for (; s + 3 < stages; ++s) {
     const int buf = s & 1;
-    const uint32_t k = (uint32_t)(s + 2) * 128;
+    const uint32_t k = (uint32_t)(s + 2) * kStep;
 #pragma unroll
     for (int ks = 0; ks < 3; ++ks) {
       read(f[(ks + 1) & 1], buf, ks + 1);
@@ -597,7 +608,7 @@ __global__ __launch_bounds__(256, BM * BN > 128 * 128 ? 1 : 2) void k_i8_tile(I8
       for (int i = 0; i < NS; ++i) write(i, buf ^ 1);
     }
     if (s + 2 < stages) {
-      const uint32_t k = (uint32_t)(s + 2) * 128 - (s + 2 == stages - 1 ? over : 0);
+      const uint32_t k = (uint32_t)(s + 2) * kStep - (s + 2 == stages - 1 ? over : 0);
 #pragma unroll
       for (int i = 0; i < NS; ++i) load(i, k);
     }
@@ -608,7 +619,18 @@ __global__ __launch_bounds__(256, BM * BN > 128 * 128 ? 1 : 2) void k_i8_tile(I8
   }
 
   __syncthreads();  // the outputs go through the same LDS
-  int8_t* mine = &lds[0][0] + wave * (int)(sizeof lds / 4);
+  int8_t* mine = &lds_all[0][0][0] + wave * (int)(sizeof lds_all / 4);
+  if constexpr (SETS == 2) {
+    int* sums = reinterpret_cast<int*>(mine) + lane;
+#pragma unroll
+    for (int x = 0; x < TM * TN * 16; ++x)
+      if (set == 1) sums[64 * x] = acc[x / 16 / TN][x / 16 % TN][x % 16];
+    __syncthreads();
+    if (set == 1) return;
+#pragma unroll
+    for (int x = 0; x < TM * TN * 16; ++x) acc[x / 16 / TN][x / 16 % TN][x % 16] += sums[64 * x];
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront", "local");
+  }
   const int64_t mw = m0 + wm, nw = n0 + wn;
   auto out = [&](auto type) {
     constexpr int T = decltype(type)::value;
@@ -646,10 +668,45 @@ void launch_rows(const void* A, int64_t M, int64_t K, int64_t lda, int8_t* Q, in
   }
 }
 
-template <int BM, int BN, bool CLAMP>
+template <int BM, int BN, bool CLAMP = false, int SETS = 1>
 void launch_tile(const I8Gemm& g, hipStream_t stream) {
   const int64_t tm = (g.M + BM - 1) / BM, tn = (g.N + BN - 1) / BN;
-  k_i8_tile<BM, BN, CLAMP><<<(unsigned)((tm * tn + 7) / 8 * 8), 256, 0, stream>>>(g, (int)tm, (int)tn);
+  k_i8_tile<BM, BN, CLAMP, SETS>
+      <<<(unsigned)((tm * tn + 7) / 8 * 8), 256 * SETS, 0, stream>>>(g, (int)tm, (int)tn);
+}
+
+// The tile of a matrix that is no smaller than it.  Larger tiles move fewer
+// bytes a product, smaller ones leave fewer CUs idle; below one tile a CU,
+// two sets of waves hide what one stage in flight does not.  Times in us of a
+// call in a graph, rows of 4096 + 128 bytes (512 in the last lines):
+//                        64x64  2 sets  64x128  2 sets  128x128  256x256
+//    65 x  4096 x 4096    10.0     9.5    12.4    11.7       -        -
+//    80 x 11008 x 4096    17.7    16.0    15.5    13.3       -        -
+//   256 x  4096 x 4096    11.3    10.4    12.9    12.2     15.9     44.9
+//   256 x 11008 x 4096    27.1    25.4    23.4    25.4     19.1     46.9
+//   512 x  4096 x 4096    21.0    18.9    16.6    16.2     18.3     46.4
+//  1024 x  4096 x 4096    36.6    33.6    26.9    28.0     22.0     47.3
+//  2048 x 11008 x 4096   151.4   158.1   124.2   147.0    101.7    113.0
+//  4096 x  4096 x 4096   112.9   117.7    92.1   108.2     74.5     67.6
+//   512 x  1024 x 1024     4.6     4.8     5.5     5.9      7.0     20.1
+//  2048 x  2048 x  512     7.2     9.0     6.8     9.2      6.8     17.2
+// So: 256x256 where it fills at least 85% of the rounds of one tile a CU that
+// it takes; else 128x128 from 160 tiles on; else 64x128 from 150 on; else
+// 64x64.  Two sets where the tiles give a CU no second one and K is long
+// enough to be shared out.
+void launch_tiles(const I8Gemm& g, hipStream_t stream) {
+  constexpr int64_t kCus = 256;
+  auto tiles = [&](int64_t bm, int64_t bn) {
+    return g.M < bm || g.N < bn ? 0 : ((g.M + bm - 1) / bm) * ((g.N + bn - 1) / bn);
+  };
+  const int64_t t256 = tiles(256, 256), t64x128 = tiles(64, 128);
+  if (t256 && 100 * t256 >= 85 * kCus * ((t256 + kCus - 1) / kCus)) launch_tile<256, 256>(g, stream);
+  else if (tiles(128, 128) >= 160) launch_tile<128, 128>(g, stream);
+  else if (t64x128 >= 150) {
+    if (t64x128 <= kCus && g.K >= 2048) launch_tile<64, 128, false, 2>(g, stream);
+    else launch_tile<64, 128>(g, stream);
+  } else if (g.K > 1024) launch_tile<64, 64, false, 2>(g, stream);
+  else launch_tile<64, 64>(g, stream);
 }
 
 // Up to 16 tokens and 8192 channels, a workgroup takes 16 channels: the
@@ -698,9 +755,7 @@ hipError_t launch_i8_gemm(const I8Gemm& g, hipStream_t stream) {
   else if (g.M <= 64) launch_skinny<8>(g, stream);
   else if (g.K < 16) k_i8_short<<<dim3((unsigned)((g.N + 255) / 256), (unsigned)std::min<int64_t>(g.M, 65535)), 256, 0, stream>>>(g);
   else if (std::max(g.lda, g.ldw) >= 1 << 24 || g.N < 64) launch_tile<64, 64, true>(g, stream);
-  else if (((g.M + 255) / 256) * ((g.N + 255) / 256) >= 200 && std::min(g.M, g.N) >= 256) launch_tile<256, 256, false>(g, stream);
-  else if (((g.M + 127) / 128) * ((g.N + 127) / 128) >= 200 && std::min(g.M, g.N) >= 128) launch_tile<128, 128, false>(g, stream);
-  else launch_tile<64, 64, false>(g, stream);
+  else launch_tiles(g, stream);
   return hipGetLastError();
 }
 

@@ -84,7 +84,9 @@ SHAPES = [  # M, N, K
     (5, 11, 127), (7, 515, 512), (8, 4096, 1024), (9, 300, 640), (16, 128, 128), (17, 17, 17), (24, 1100, 96),
     (33, 4099, 257), (40, 256, 4096), (48, 33, 8192), (63, 65, 63), (64, 64, 64), (65, 129, 191), (100, 768, 768),
     (128, 128, 4096), (129, 257, 385), (200, 2304, 768), (256, 256, 256), (257, 511, 1000), (301, 199, 4091),
-    (513, 1025, 129), (1000, 300, 2048), (2049, 140, 320), (1, 70000, 64), (4097, 65, 64), (512, 2560, 1152)]
+    (513, 1025, 129), (1000, 300, 2048), (2049, 140, 320), (1, 70000, 64), (4097, 65, 64), (512, 2560, 1152),
+    (130, 1300, 2065), (100, 10000, 2049), (70, 19300, 130), (2050, 1300, 100), (300, 9000, 1000), (3900, 4100, 200),
+    (66, 64, 1025), (64, 9999, 16), (200, 64, 15), (90, 30, 2000), (8200, 260, 16)]
 
 
 @pytest.mark.parametrize("M,N,K", SHAPES, ids=lambda v: str(v))
