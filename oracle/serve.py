@@ -144,10 +144,10 @@ def attention(q, kc, ks, vc, vs, table, cu, kv_len, bits, scale, mask=None):
                         p = e / e.sum()
                         out[t, h * G + g] = p @ V
                         lse[t, h * G + g] = m + np.log(e.sum())
-                        size = scale * (np.abs(K) @ np.abs(x))
+                        size = abs(scale) * (np.abs(K) @ np.abs(x))
                         ds = (D + 16) * 2.0**-24 * size.max() + 8 * 2.0**-24 * (1 + np.abs(z).max())
                         # the fp16 grid of q: relative to the row's largest element
-                        ds += scale * 2.0**-24 * np.abs(x).max(initial=0) * np.abs(K).sum(1).max()
+                        ds += abs(scale) * 2.0**-24 * np.abs(x).max(initial=0) * np.abs(K).sum(1).max()
                         A = p @ np.abs(V)
                         top = (p * sv[seen, h]).max() * np.abs(cv[seen, h]).sum(0)
                         bound[t, h * G + g] = A * (2.0**-11 + 2 * ds + len(z) * 2.0**-24) + 2.0**-25 * top

@@ -164,20 +164,19 @@ __global__ __launch_bounds__(256) void k_kv_copy(KvCopy c, int tw) {
 // Queries are scaled by a power of two per row to use fp16's whole range
 // (bf16 queries are exact in it down to 2^-22 of the row's largest element).
 //
-// Softmax of row r over the positions so far, all in fp32:
-//   m  a value near the largest score (base 2), l = sum exp2(s - m);
-//   w  = exp2(s - m) * s_v / sg, the weight rounded to fp16 for the product,
-//   sg = a value near the largest exp2(s - m) * s_v, so that a weight is off
-//        by at most half a step of fp16 whatever the V scales' range.
-// The accumulators hold O / sg.  m and sg move only when a new value passes
-// them by 2^6 or 2^8 (fp16 has room), so rescaling is rare; a new m scales
-// l and sg alone.
+// Softmax of a row over the positions so far, all in fp32 and base 2, has one
+// reference r for the sum and the weights:
+//   l = sum exp2(s - r),  w = exp2(s - r) * s_v,  outputs = sum w * code.
+// w is rounded to fp16 for the product, so r is chosen by the weights: the
+// largest w so far is near 1 (`ref`), and r moves only when one passes it by
+// 2^8 (fp16 has room) or an exponential nears fp32's end.  So a weight is off
+// by at most half a step of fp16 whatever the range of the V scales, down to
+// s_v = 2^-60 of the row's largest exp2(s - r), and rescaling is rare.
 typedef _Float16 h2 __attribute__((ext_vector_type(2)));
 typedef _Float16 h8 __attribute__((ext_vector_type(8)));
 typedef float f4 __attribute__((ext_vector_type(4)));
 
 constexpr int kSub = 1024;     // positions whose rows and scales LDS holds at a time
-constexpr float kSgMin = 0x1p-120f;
 
 // Over the four lanes that share c: the same result in each.
 __device__ __forceinline__ float quad_max(float x) {
@@ -195,6 +194,61 @@ __device__ __forceinline__ float quad_sum(float x) {
   const uint32_t v = __float_as_uint(x);
   const auto b = __builtin_amdgcn_permlane32_swap(v, v, false, false);
   return __uint_as_float(b[0]) + __uint_as_float(b[1]);
+}
+
+// One step of a row's softmax over N positions a lane.  x: scores without the
+// row's unit qf (positive), -inf at hidden positions, where v is 0.  Leaves
+// the weights in x, and calls scale(f) where the outputs so far have to be
+// multiplied.  A row starts at r = kHidden, where a visible score's exponential
+// is infinite and a hidden one's 0, and stays there while it sees nothing.
+constexpr float kHidden = -3e38f;
+struct RowSoftmax {
+  float r, l, ref;
+};
+template <int N, class Scale>
+__device__ __forceinline__ void softmax_step(float (&x)[N], const float (&v)[N], float qf, RowSoftmax& st, Scale scale) {
+  float w[N], lt, top;
+  auto weigh = [&]() {
+    lt = 0.0f, top = 0.0f;
+#pragma unroll
+    for (int e = 0; e < N; ++e) {
+      const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(x[e], qf, -st.r));
+      lt += p;
+      w[e] = p * v[e];
+      top = fmaxf(top, fabsf(w[e]));
+    }
+  };
+  weigh();
+  if (__any(lt > 0x1p80f || top > 256.0f * st.ref)) {
+    float mx = x[0];
+#pragma unroll
+    for (int e = 1; e < N; ++e) mx = fmaxf(mx, x[e]);
+    mx = quad_max(mx * qf);
+    float f = 1.0f;
+    if (mx > st.r + 80.0f) {  // the first positions, or scores far above those before
+      f = __builtin_amdgcn_exp2f(st.r - mx);
+      st.r = mx;
+    }
+    weigh();
+    top = quad_max(top);
+    float up = 1.0f;
+    if (top > 256.0f * (st.ref * f)) {
+      const int e = max((int)(__float_as_uint(top) >> 23) - 127, -60);
+      up = __uint_as_float((uint32_t)(127 - min(e, 126)) << 23);
+      st.r += (float)min(e, 126);
+      st.ref = top * up;
+    } else {
+      st.ref *= f;
+    }
+    st.l *= f * up;
+    lt *= up;
+#pragma unroll
+    for (int e = 0; e < N; ++e) w[e] *= up;
+    scale(f * up);
+  }
+  st.l += lt;
+#pragma unroll
+  for (int e = 0; e < N; ++e) x[e] = w[e];
 }
 
 // Two V codes moved to unsigned, times 2^-9.
@@ -314,10 +368,12 @@ struct KvLds {
 };
 
 // Waves a SIMD, by the registers that a row tile's outputs take.
-constexpr int kv_waves(int D, int R) { return D * R <= 128 ? 4 : D == 128 ? 3 : 2; }
+constexpr int kv_waves(int D, int BITS, int R) {
+  return D * R <= 64 || (D == 128 && R == 1 && BITS == 4) ? 4 : D * R <= 128 || (D == 128 && BITS == 4) ? 3 : 2;
+}
 
 template <int D, int BITS, int R>
-__global__ __launch_bounds__(256, kv_waves(D, R)) void k_kv_attend(KvAttend a, KvSplit sp) {
+__global__ __launch_bounds__(256, kv_waves(D, BITS, R)) void k_kv_attend(KvAttend a, KvSplit sp) {
   constexpr int RB = D * BITS / 8;   // bytes of a cache row
   constexpr int KB = RB / 4, VB = RB / 16;
   constexpr int NK = D / 32;         // products over d
@@ -402,19 +458,20 @@ __global__ __launch_bounds__(256, kv_waves(D, R)) void k_kv_attend(KvAttend a, K
 #pragma unroll
     for (int o = 1; o < TPR; o *= 2) sum += __shfl_xor(sum, o);
     if (tid % TPR == 0) {
-      L.qf[qr] = fabsf(a.scale) * 1.44269504f * 0x1p24f * __uint_as_float((uint32_t)(127 + e) << 23);
+      // (never 0: hidden positions stay at -inf)
+      L.qf[qr] = fmaxf(fabsf(a.scale) * 1.44269504f * 0x1p24f * __uint_as_float((uint32_t)(127 + e) << 23), 0x1p-126f);
       L.qz[qr] = sum * (BITS == 8 ? -0x1p-17f : -0x1p-21f);
       L.qi[qr] = qr < rows ? (row0 + qr) / G : -1;
     }
   };
 
   f4 O[R][DB];
-  float m[R], l[R], sg[R], inv[R];
+  RowSoftmax sm[R];
 #pragma unroll
   for (int rt = 0; rt < R; ++rt) {
 #pragma unroll
     for (int j = 0; j < DB; ++j) O[rt][j] = f4{0.0f, 0.0f, 0.0f, 0.0f};
-    m[rt] = -INFINITY, l[rt] = 0.0f, sg[rt] = 0.0f, inv[rt] = 0.0f;
+    sm[rt] = {kHidden, 0.0f, 0.0f};
   }
 
   const uint8_t* kp = a.k + kb * KB;
@@ -529,42 +586,12 @@ __global__ __launch_bounds__(256, kv_waves(D, R)) void k_kv_attend(KvAttend a, K
             v[e] = on ? v[e] : 0.0f;
           }
         }
-        float mx = s[0];
+        softmax_step<8>(s, v, qf, sm[rt], [&](float f) {
 #pragma unroll
-        for (int e = 1; e < 8; ++e) mx = fmaxf(mx, s[e]);
-        mx *= qf;
-        if (__any(mx > m[rt] + 6.0f)) {
-          mx = quad_max(mx);
-          const float mn = mx > m[rt] + 6.0f ? mx : m[rt];
-          const float al = mn == m[rt] ? 1.0f : __builtin_amdgcn_exp2f(m[rt] - mn);
-          m[rt] = mn;
-          l[rt] *= al;
-          sg[rt] *= al;
-          sg[rt] = sg[rt] < kSgMin ? 0.0f : sg[rt];
-          inv[rt] = sg[rt] > 0.0f ? __builtin_amdgcn_rcpf(sg[rt]) : 0.0f;
-        }
-        const float mu = m[rt] == -INFINITY ? 0.0f : m[rt];
-        float top = 0.0f;
+          for (int j = 0; j < DB; ++j) O[rt][j] *= f;
+        });
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(s[e], qf, -mu));
-          l[rt] += p;
-          s[e] = p * v[e];
-          top = fmaxf(top, fabsf(s[e]));
-        }
-        if (__any(top > 256.0f * sg[rt])) {
-          top = quad_max(top);
-          if (top > 256.0f * sg[rt]) {
-            const float ns = fmaxf(top, kSgMin);
-            inv[rt] = __builtin_amdgcn_rcpf(ns);
-            const float f = sg[rt] * inv[rt];
-            sg[rt] = ns;
-#pragma unroll
-            for (int j = 0; j < DB; ++j) O[rt][j] *= f;
-          }
-        }
-#pragma unroll
-        for (int e = 0; e < 8; ++e) P[rt][e] = (_Float16)(s[e] * inv[rt]);
+        for (int e = 0; e < 8; ++e) P[rt][e] = (_Float16)s[e];
       }
 
       // O^T += V^T P^T, one element of d per lane column at a time
@@ -607,16 +634,14 @@ __global__ __launch_bounds__(256, kv_waves(D, R)) void k_kv_attend(KvAttend a, K
 #pragma unroll
   for (int rt = 0; rt < R; ++rt) {
     __syncthreads();
-    const float ls = quad_sum(l[rt]);
+    const float ls = quad_sum(sm[rt].l);
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       float* o = out + (wave * 16 + c) * OP + (4 * kb + i) * DB;
 #pragma unroll
       for (int j = 0; j < DB; ++j) o[j] = O[rt][j][i];
     }
-    if (kb == 0) ml[(wave * 16 + c) * 2] = m[rt], ml[(wave * 16 + c) * 2 + 1] = ls;
-    // their unit (the codes were taken times 2^-9) in the row's first padding element
-    if (kb == 0) out[(wave * 16 + c) * OP + D] = sg[rt] * 512.0f;
+    if (kb == 0) ml[(wave * 16 + c) * 2] = sm[rt].r, ml[(wave * 16 + c) * 2 + 1] = ls;
     __syncthreads();
     for (int x = tid; x < 16 * (D / 4); x += 256) {
       const int r = x / (D / 4), d = x % (D / 4) * 4, rr = row0 + 16 * rt + r;
@@ -625,13 +650,13 @@ __global__ __launch_bounds__(256, kv_waves(D, R)) void k_kv_attend(KvAttend a, K
 #pragma unroll
       for (int w = 0; w < 4; ++w) M = fmaxf(M, ml[(w * 16 + r) * 2]);
       const float mu = M == -INFINITY ? 0.0f : M;
-      float sum = 0.0f, f[4];
+      float sum = 0.0f, f[4];  // the outputs' codes were taken times 2^-9
       f4 o = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
       for (int w = 0; w < 4; ++w) {
         const float e = __builtin_amdgcn_exp2f(ml[(w * 16 + r) * 2] - mu);
         sum += ml[(w * 16 + r) * 2 + 1] * e;
-        f[w] = out[(w * 16 + r) * OP + D] * e;
+        f[w] = 512.0f * e;
       }
       const float by = direct ? (sum == 0.0f ? 0.0f : 1.0f / sum) : 1.0f;
 #pragma unroll

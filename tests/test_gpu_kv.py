@@ -251,6 +251,18 @@ def test_what_is_masked_cannot_be_seen(bits):
             assert (np.abs(got[t] - want[t]) <= bound[t] + 2.0**-8 * (np.abs(want[t]) + bound[t])).all()
 
 
+@pytest.mark.parametrize("scale", [0.0, -0.125])
+def test_scales_of_zero_and_below(scale):
+    """A scale of 0 averages what is visible; a negative one turns the order."""
+    r = np.random.default_rng(15)
+    lens = [70, 9]
+    pages, table = _tables(r, lens, 16)
+    cache, h = _random_cache(r, pages, 16, 2, 64, 8)
+    q = torch.from_numpy(r.standard_normal((6, 4, 64)).astype(np.float32)).to(torch.bfloat16).cuda()
+    q[1] = 0
+    _check_attention(cache, h, q, table, [0, 3, 6], lens, 8, scale=scale)
+
+
 def test_extreme_scores_and_scales():
     """Scores that leave one position, V scales that span 2^40 and fall where
     the weights rise, q rows that span fp16's range and beyond."""
