@@ -316,6 +316,29 @@ struct Raw {
   }
 };
 
+// A lane's V codes moved to unsigned, and from eight positions of them the
+// operand of its element j.
+template <int VB, int BITS>
+__device__ __forceinline__ void v_unsigned(Raw<VB>& r) {
+#pragma unroll
+  for (int i = 0; i < (VB + 3) / 4; ++i) r.w[i] ^= BITS == 8 ? 0x80808080u : 0x88888888u;
+}
+template <int VB, int BITS>
+__device__ __forceinline__ h8 v_operand(const Raw<VB> (&r)[8], int j) {
+  union { h2 p[4]; h8 v; } x;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    uint32_t lo = r[2 * i].w[j * BITS / 32], hi = r[2 * i + 1].w[j * BITS / 32];
+    if constexpr (BITS == 4) {
+      lo = (lo >> (4 * (j & 1))) & 0x0F0F0F0Fu;
+      hi = (hi >> (4 * (j & 1))) & 0x0F0F0F0Fu;
+    }
+    const uint32_t by = j * BITS / 8 % 4;
+    x.p[i] = v_half<BITS>(__builtin_amdgcn_perm(hi, lo, 0x0c000c00u | (4 + by) << 16 | by));
+  }
+  return x.v;
+}
+
 // Which of the 32 positions from new position j0 on (negative: older ones)
 // new query i of ragged row t sees.
 __device__ __forceinline__ uint32_t seen_bits(const KvAttend& a, int64_t t, int i, int64_t j0) {
@@ -357,14 +380,148 @@ __device__ __forceinline__ KvPart part_of(int len, int part, int parts, int chun
   return {(int)first, count, (int)(((uint32_t)len + c - 1) / c)};
 }
 
-template <int D, int R>
-struct KvLds {
+// What a workgroup works on.
+struct KvUnit {
+  KvSpan span;    // the sequence's rows of the ragged batch
+  int nq, len;    // its queries that are computed, its positions
+  int64_t base;   // its positions before the new ones (may be negative)
+  int b, h, part, row0, rows;  // row0, rows: query rows (query * group + head) of this workgroup
+  KvPart pt;
+};
+// Workgroups of the same positions go to one XCD, one after the other.
+// False: there is nothing to do.
+__device__ __forceinline__ bool kv_unit(const KvAttend& a, const KvSplit& sp, KvUnit& u) {
+  const uint32_t id = blockIdx.x, x = id / 8;
+  const int rb = (int)(x % sp.RB), unit = (int)(x / sp.RB) * 8 + (int)(id % 8);
+  const int bp = unit / a.dims.heads;
+  u.h = unit % a.dims.heads;
+  u.part = bp % sp.parts, u.b = bp / sp.parts;
+  if (u.b >= a.table.B) return false;
+  u.span = kv_span(a.cu[u.b], a.cu[u.b + 1], a.T);
+  u.nq = min(u.span.count, a.max_q);
+  u.len = kv_length(a.table, a.dims, a.kv_len[u.b]);
+  u.base = (int64_t)a.kv_len[u.b] - u.span.count;
+  u.row0 = rb * 16 * sp.R;
+  u.rows = min(u.nq * a.group - u.row0, 16 * sp.R);
+  u.pt = part_of(u.len, u.part, sp.parts, sp.chunk);
+  return u.rows > 0 && (u.part == 0 || u.pt.count > 0);
+}
+
+// Per query row: the unit of its scores, where they start, its query (-1: none).
+template <int ROWS>
+struct KvRowInfo {
+  float qf[ROWS], qz[ROWS];
+  int32_t qi[ROWS];
+};
+
+// The queries of 16 * R rows on their way to LDS as operands: loaded before
+// anything waits, turned once the K and V loads are out.
+template <int D, int BITS, int R>
+struct KvQuery {
+  // threads a row: a power of two that leaves each a multiple of 8 elements
+  static constexpr int kMost = D % 128 == 0 ? 16 : 8, TPR = 16 / R < kMost ? 16 / R : kMost, PER = D / TPR;
+  struct __attribute__((packed, aligned(2))) P { uint16_t v[8]; };
+  P raw[PER / 8];
+  __device__ __forceinline__ void load(const KvAttend& a, const KvUnit& u, int tid) {
+    const int r = tid / TPR, d = tid % TPR * PER;
+    if (r < u.rows) {  // rows <= 16 R: the threads past them have none
+      const int64_t t = u.span.first + (u.row0 + r) / a.group;
+      const int64_t at = t * a.q_ts + ((int64_t)u.h * a.group + (u.row0 + r) % a.group) * a.q_hs + d;
+      const uint16_t* p = static_cast<const uint16_t*>(a.q) + at;
+#pragma unroll
+      for (int g = 0; g < PER / 8; ++g) raw[g] = *reinterpret_cast<const P*>(p + 8 * g);
+    } else {
+#pragma unroll
+      for (int g = 0; g < PER / 8; ++g)
+#pragma unroll
+        for (int i = 0; i < 8; ++i) raw[g].v[i] = 0;
+    }
+  }
+  __device__ __forceinline__ void stage(const KvAttend& a, const KvUnit& u, int tid, h8 (*q)[D / 32][64],
+                                        KvRowInfo<16 * R>& info) const {
+    if (tid >= 16 * R * TPR) return;
+    const int r = tid / TPR, d0 = tid % TPR * PER;
+    auto value = [&](int i) {
+      const uint16_t x = raw[i / 8].v[i % 8];
+      return a.type == SONIQ_BF16 ? bf16_value(x) : (float)__builtin_bit_cast(_Float16, x);
+    };
+    uint32_t mx = 0;
+#pragma unroll
+    for (int i = 0; i < PER; ++i) mx = max(mx, __float_as_uint(value(i)) & 0x7FFFFFFFu);
+#pragma unroll
+    for (int o = 1; o < TPR; o *= 2) mx = max(mx, (uint32_t)__shfl_xor((int)mx, o));
+    // largest element to [2^14, 2^15); rows of zeros, infinities or NaN as they are
+    int e = (int)(mx >> 23) - 127 - 14;
+    e = mx >= 0x7F800000u || mx == 0 ? 0 : max(e, -100);
+    const float down = copysignf(__uint_as_float((uint32_t)(127 - e) << 23), a.scale);
+    float sum = 0.0f;
+#pragma unroll
+    for (int g = 0; g < PER / 8; ++g) {
+      h8 v;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const _Float16 y = (_Float16)(value(8 * g + i) * down);
+        v[k_order<BITS>(i)] = y;
+        sum += (float)y;
+      }
+      const int d = d0 + 8 * g;
+      q[r / 16][d % (D / 4) / 8][d / (D / 4) * 16 + r % 16] = v;
+    }
+#pragma unroll
+    for (int o = 1; o < TPR; o *= 2) sum += __shfl_xor(sum, o);
+    if (tid % TPR == 0) {
+      // (never 0: hidden positions stay at -inf)
+      info.qf[r] = fmaxf(fabsf(a.scale) * 1.44269504f * 0x1p24f * __uint_as_float((uint32_t)(127 + e) << 23), 0x1p-126f);
+      info.qz[r] = sum * (BITS == 8 ? -0x1p-17f : -0x1p-21f);
+      info.qi[r] = r < u.rows ? (u.row0 + r) / a.group : -1;
+    }
+  }
+};
+
+// Positions [p0, p0 + n) of a sequence, n <= kSub, in LDS: cache row, scales,
+// validity (a position without a page has row 0 and a clear bit).
+struct KvPositions {
   uint32_t row[kSub];
   float ks[kSub], vs[kSub];
   uint32_t valid[kSub / 32];
+};
+struct KvFind {
+  int32_t at[kSub / 256];
+  float ks[kSub / 256], vs[kSub / 256];
+  __device__ __forceinline__ void find(const KvAttend& a, const KvUnit& u, int p0, int n, int tid) {
+#pragma unroll
+    for (int k = 0; k < kSub / 256; ++k) {
+      const int x = tid + 256 * k;
+      at[k] = x < n ? kv_row(a.table, a.dims, u.b, (int64_t)p0 + x) : -1;
+    }
+  }
+  __device__ __forceinline__ void rows(const KvAttend& a, const KvUnit& u, int n, int tid, KvPositions& L) {
+#pragma unroll
+    for (int k = 0; k < kSub / 256; ++k) {
+      const int x = tid + 256 * k;
+      ks[k] = vs[k] = 0.0f;
+      if (256 * k < n) {
+        const uint64_t there = __ballot(at[k] >= 0);
+        if (tid % 64 == 0) L.valid[x / 32] = (uint32_t)there;
+        if (tid % 64 == 32) L.valid[x / 32] = (uint32_t)(there >> 32);
+        const int32_t row = at[k] < 0 ? 0 : at[k] + u.h * a.dims.page_size;
+        L.row[x] = row;
+        ks[k] = a.ks[row], vs[k] = a.vs[row];
+      }
+    }
+  }
+  __device__ __forceinline__ void scales(int n, int tid, KvPositions& L) const {
+#pragma unroll
+    for (int k = 0; k < kSub / 256; ++k)
+      if (256 * k < n) L.ks[tid + 256 * k] = ks[k], L.vs[tid + 256 * k] = vs[k];
+  }
+};
+
+template <int D, int R>
+struct KvLds {
+  KvPositions p;
   h8 q[R][D / 32][64];
-  float qf[16 * R], qz[16 * R];  // per row: unit of the scores, and where they start
-  int32_t qi[16 * R];            // per row: its query, -1 for none
+  KvRowInfo<16 * R> info;
 };
 
 // Waves a SIMD, by the registers that a row tile's outputs take.
@@ -383,87 +540,14 @@ __global__ __launch_bounds__(256, kv_waves(D, BITS, R)) void k_kv_attend(KvAtten
   __shared__ __align__(16) uint8_t lds_bytes[kLdsLoop > kLdsOut ? kLdsLoop : kLdsOut];
   KvLds<D, R>& L = *reinterpret_cast<KvLds<D, R>*>(lds_bytes);
 
-  // workgroups of the same positions go to one XCD, one after the other
-  const int H = a.dims.heads, G = a.group;
-  int rb, u;
-  {
-    const uint32_t id = blockIdx.x, x = id / 8;
-    rb = (int)(x % sp.RB);
-    u = (int)(x / sp.RB) * 8 + (int)(id % 8);
-  }
-  const int h = u % H, bp = u / H, part = bp % sp.parts, b = bp / sp.parts;
-  if (b >= a.table.B) return;
-  const KvSpan span = kv_span(a.cu[b], a.cu[b + 1], a.T);
-  const int nq = min(span.count, a.max_q);
-  const int len = kv_length(a.table, a.dims, a.kv_len[b]);
-  const int64_t base = (int64_t)a.kv_len[b] - span.count;
-  const int row0 = rb * 16 * R, rows = min(nq * G - row0, 16 * R);
-  const KvPart pt = part_of(len, part, sp.parts, sp.chunk);
-  if (rows <= 0 || (part > 0 && pt.count == 0)) return;
-
+  KvUnit un;
+  if (!kv_unit(a, sp, un)) return;
+  const int h = un.h, G = a.group, nq = un.nq, row0 = un.row0;
+  const KvSpan span = un.span;
+  const KvPart pt = un.pt;
+  const int64_t base = un.base;
   const int tid = threadIdx.x, lane = tid % 64, c = lane % 16, kb = lane / 16;
   const int wave = __builtin_amdgcn_readfirstlane(tid / 64);  // uniform, and known to be
-
-  // ---- the queries' loads go out before anything waits; they become operands
-  // while the first K and V are on their way
-  // threads a row: a power of two that leaves each a multiple of 8 elements
-  constexpr int kMost = D % 128 == 0 ? 16 : 8, TPR = 16 / R < kMost ? 16 / R : kMost;
-  constexpr int PER = D / TPR;
-  struct __attribute__((packed, aligned(2))) QP { uint16_t v[8]; };
-  QP qraw[PER / 8];
-  const int qr = tid / TPR, qd = tid % TPR * PER;
-  auto load_q = [&]() {
-    if (qr < rows) {  // rows <= 16 R: the threads past them have none
-      const int64_t t = span.first + (row0 + qr) / G;
-      const int64_t at = t * a.q_ts + ((int64_t)h * G + (row0 + qr) % G) * a.q_hs + qd;
-      const uint16_t* p = static_cast<const uint16_t*>(a.q) + at;
-#pragma unroll
-      for (int g = 0; g < PER / 8; ++g) qraw[g] = *reinterpret_cast<const QP*>(p + 8 * g);
-    } else {
-#pragma unroll
-      for (int g = 0; g < PER / 8; ++g)
-#pragma unroll
-        for (int i = 0; i < 8; ++i) qraw[g].v[i] = 0;
-    }
-  };
-  auto stage_q = [&]() {
-    if (tid >= 16 * R * TPR) return;
-    float x[PER];
-    uint32_t mx = 0;
-#pragma unroll
-    for (int i = 0; i < PER; ++i) {
-      const uint16_t u = qraw[i / 8].v[i % 8];
-      x[i] = a.type == SONIQ_BF16 ? bf16_value(u) : (float)__builtin_bit_cast(_Float16, u);
-      mx = max(mx, __float_as_uint(x[i]) & 0x7FFFFFFFu);
-    }
-#pragma unroll
-    for (int o = 1; o < TPR; o *= 2) mx = max(mx, (uint32_t)__shfl_xor((int)mx, o));
-    // largest element to [2^14, 2^15); rows of zeros, infinities or NaN as they are
-    int e = (int)(mx >> 23) - 127 - 14;
-    e = mx >= 0x7F800000u || mx == 0 ? 0 : max(e, -100);
-    const float down = copysignf(__uint_as_float((uint32_t)(127 - e) << 23), a.scale);
-    float sum = 0.0f;
-#pragma unroll
-    for (int g = 0; g < PER / 8; ++g) {
-      h8 v;
-#pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        const _Float16 y = (_Float16)(x[8 * g + i] * down);
-        v[k_order<BITS>(i)] = y;
-        sum += (float)y;
-      }
-      const int d = qd + 8 * g;
-      L.q[qr / 16][d % (D / 4) / 8][d / (D / 4) * 16 + qr % 16] = v;
-    }
-#pragma unroll
-    for (int o = 1; o < TPR; o *= 2) sum += __shfl_xor(sum, o);
-    if (tid % TPR == 0) {
-      // (never 0: hidden positions stay at -inf)
-      L.qf[qr] = fmaxf(fabsf(a.scale) * 1.44269504f * 0x1p24f * __uint_as_float((uint32_t)(127 + e) << 23), 0x1p-126f);
-      L.qz[qr] = sum * (BITS == 8 ? -0x1p-17f : -0x1p-21f);
-      L.qi[qr] = qr < rows ? (row0 + qr) / G : -1;
-    }
-  };
 
   f4 O[R][DB];
   RowSoftmax sm[R];
@@ -480,12 +564,12 @@ __global__ __launch_bounds__(256, kv_waves(D, BITS, R)) void k_kv_attend(KvAtten
   Raw<VB> vr[8];
   auto load_k = [&](int st) {
 #pragma unroll
-    for (int t = 0; t < 2; ++t) kr[t].load(kp + (uint64_t)L.row[st * 32 + 16 * t + c] * RB);
+    for (int t = 0; t < 2; ++t) kr[t].load(kp + (uint64_t)L.p.row[st * 32 + 16 * t + c] * RB);
   };
   auto load_v = [&](int st) {
 #pragma unroll
     for (int t = 0; t < 2; ++t) {
-      const uint4 x = *reinterpret_cast<const uint4*>(&L.row[st * 32 + 16 * t + 4 * kb]);
+      const uint4 x = *reinterpret_cast<const uint4*>(&L.p.row[st * 32 + 16 * t + 4 * kb]);
       vr[4 * t].load(vp + (uint64_t)x.x * RB);
       vr[4 * t + 1].load(vp + (uint64_t)x.y * RB);
       vr[4 * t + 2].load(vp + (uint64_t)x.z * RB);
@@ -493,41 +577,22 @@ __global__ __launch_bounds__(256, kv_waves(D, BITS, R)) void k_kv_attend(KvAtten
     }
   };
 
-  // Cache rows, validity and scales of positions [s0, s0 + kSub) of the part
-  // into LDS, with this wave's first K and V on their way.
+  // Positions [s0, s0 + kSub) of the part into LDS, with this wave's first K
+  // and V on their way.
   auto prepare = [&](int s0, auto first) {
-    const int n = min(pt.count - s0, kSub), p0 = pt.first + s0;
-    float kreg[kSub / 256], vreg[kSub / 256];
-    int32_t at[kSub / 256];
-#pragma unroll
-    for (int k = 0; k < kSub / 256; ++k) {
-      const int x = tid + 256 * k;
-      at[k] = x < n ? kv_row(a.table, a.dims, b, (int64_t)p0 + x) : -1;
-    }
-    if constexpr (decltype(first)::value) load_q();
-#pragma unroll
-    for (int k = 0; k < kSub / 256; ++k) {
-      const int x = tid + 256 * k;
-      kreg[k] = vreg[k] = 0.0f;
-      if (256 * k < n) {
-        int32_t row = at[k];
-        const uint64_t there = __ballot(row >= 0);
-        if (lane == 0) L.valid[x / 32] = (uint32_t)there;
-        if (lane == 32) L.valid[x / 32] = (uint32_t)(there >> 32);
-        row = row < 0 ? 0 : row + h * a.dims.page_size;
-        L.row[x] = row;
-        kreg[k] = a.ks[row], vreg[k] = a.vs[row];
-      }
-    }
+    const int n = min(pt.count - s0, kSub);
+    KvFind f;
+    KvQuery<D, BITS, R> q;
+    f.find(a, un, pt.first + s0, n, tid);
+    if constexpr (decltype(first)::value) q.load(a, un, tid);
+    f.rows(a, un, n, tid, L.p);
     lds_barrier();
     if (wave < (n + 31) / 32) {
       load_k(wave);
       load_v(wave);
     }
-    if constexpr (decltype(first)::value) stage_q();
-#pragma unroll
-    for (int k = 0; k < kSub / 256; ++k)
-      if (256 * k < n) L.ks[tid + 256 * k] = kreg[k], L.vs[tid + 256 * k] = vreg[k];
+    if constexpr (decltype(first)::value) q.stage(a, un, tid, L.q, L.info);
+    f.scales(n, tid, L.p);
     lds_barrier();
   };
 
@@ -541,7 +606,7 @@ __global__ __launch_bounds__(256, kv_waves(D, BITS, R)) void k_kv_attend(KvAtten
       for (int rt = 0; rt < R; ++rt) {
         int x = 16 * rt + c;
         asm volatile("" : "+v"(x));
-        const float z = L.qz[x];
+        const float z = L.info.qz[x];
         S[rt][0] = S[rt][1] = f4{z, z, z, z};
       }
 #pragma unroll
@@ -558,7 +623,7 @@ __global__ __launch_bounds__(256, kv_waves(D, BITS, R)) void k_kv_attend(KvAtten
       }
       if (more) load_k(st + 4);
 
-      const uint32_t valid = __builtin_amdgcn_readfirstlane(L.valid[st]);
+      const uint32_t valid = __builtin_amdgcn_readfirstlane(L.p.valid[st]);
       const int64_t j0 = (int64_t)p0 + st * 32 - base;
       const bool whole = valid == ~0u && j0 <= -32;
       h8 P[R];
@@ -567,9 +632,9 @@ __global__ __launch_bounds__(256, kv_waves(D, BITS, R)) void k_kv_attend(KvAtten
         if constexpr (R > 1) __builtin_amdgcn_sched_barrier(0);
         int x = 16 * rt + c, y = st * 32 + 4 * kb;
         asm volatile("" : "+v"(x), "+v"(y));  // read here: nothing of this is kept over the row tiles
-        const float qf = L.qf[x];
-        const f4 ks0 = *reinterpret_cast<const f4*>(&L.ks[y]), ks1 = *reinterpret_cast<const f4*>(&L.ks[y + 16]);
-        const f4 vs0 = *reinterpret_cast<const f4*>(&L.vs[y]), vs1 = *reinterpret_cast<const f4*>(&L.vs[y + 16]);
+        const float qf = L.info.qf[x];
+        const f4 ks0 = *reinterpret_cast<const f4*>(&L.p.ks[y]), ks1 = *reinterpret_cast<const f4*>(&L.p.ks[y + 16]);
+        const f4 vs0 = *reinterpret_cast<const f4*>(&L.p.vs[y]), vs1 = *reinterpret_cast<const f4*>(&L.p.vs[y + 16]);
         float s[8], v[8];
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
@@ -577,7 +642,7 @@ __global__ __launch_bounds__(256, kv_waves(D, BITS, R)) void k_kv_attend(KvAtten
           v[i] = vs0[i], v[4 + i] = vs1[i];
         }
         if (!whole) {
-          const int i = L.qi[x];
+          const int i = L.info.qi[x];
           const uint32_t bits = (i >= 0 ? valid & seen_bits(a, span.first + i, i, j0) : 0u) >> (4 * kb);
 #pragma unroll
           for (int e = 0; e < 8; ++e) {
@@ -597,26 +662,13 @@ __global__ __launch_bounds__(256, kv_waves(D, BITS, R)) void k_kv_attend(KvAtten
       // O^T += V^T P^T, one element of d per lane column at a time
       if constexpr (R > 1) __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-      for (int e = 0; e < 8; ++e)
-#pragma unroll
-        for (int i = 0; i < (VB + 3) / 4; ++i) vr[e].w[i] ^= BITS == 8 ? 0x80808080u : 0x88888888u;
+      for (int e = 0; e < 8; ++e) v_unsigned<VB, BITS>(vr[e]);
 #pragma unroll
       for (int j = 0; j < DB; ++j) {
-        if constexpr (D * R > 256) __builtin_amdgcn_sched_barrier(0);
-        union { h2 p[4]; h8 v; } x;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          uint32_t lo = vr[2 * i].w[j * BITS / 32], hi = vr[2 * i + 1].w[j * BITS / 32];
-          if constexpr (BITS == 4) {
-            lo = (lo >> (4 * (j & 1))) & 0x0F0F0F0Fu;
-            hi = (hi >> (4 * (j & 1))) & 0x0F0F0F0Fu;
-          }
-          const uint32_t by = j * BITS / 8 % 4;
-          x.p[i] = v_half<BITS>(__builtin_amdgcn_perm(hi, lo, 0x0c000c00u | (4 + by) << 16 | by));
-        }
+        const h8 x = v_operand<VB, BITS>(vr, j);
 #pragma unroll
         for (int rt = 0; rt < R; ++rt)
-          O[rt][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(x.v, P[rt], O[rt][j], 0, 0, 0);
+          O[rt][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(x, P[rt], O[rt][j], 0, 0, 0);
       }
       if (more) load_v(st + 4);
     }
@@ -673,7 +725,7 @@ __global__ __launch_bounds__(256, kv_waves(D, BITS, R)) void k_kv_attend(KvAtten
         if (d == 0 && a.lse)
           a.lse[t * a.q_heads + hq] = sum == 0.0f ? -INFINITY : (M + __log2f(sum)) * 0.693147181f;
       } else {
-        const int64_t x = (t * a.q_heads + hq) * sp.parts + part;
+        const int64_t x = (t * a.q_heads + hq) * sp.parts + un.part;
         *reinterpret_cast<f4*>(a.work + x * D + d) = o;
         if (d == 0) ml_out[2 * x] = M, ml_out[2 * x + 1] = sum;
       }
@@ -757,11 +809,15 @@ __global__ __launch_bounds__(256) void k_kv_join(KvAttend a, KvSplit sp) {
 // Rows a workgroup takes, and how the positions are cut.  At least about a
 // thousand workgroups where the positions give them (two to four a CU are
 // resident), at most about eight thousand, and parts of at most 1024
-// positions a row tile otherwise, so that ragged lengths level out.
+// positions a row tile otherwise, so that ragged lengths level out.  A part
+// costs its workgroup a start of several dependent loads, and 4 bytes an
+// output written and read again (eight sequences of 3001 to 8191 positions,
+// 8 heads, 96 rows: 62 us with a target of 1024 workgroups, 66 with 2048, 78
+// with 4096; 512 rows: 192, 188, 187).  Four row tiles a wave spill.
 KvSplit kv_split(const KvDims& d, int32_t q_heads, int64_t B, int64_t max_q, int64_t max_kv) {
   const int64_t rows = max_q * (q_heads / d.heads);
   KvSplit s;
-  s.R = rows <= 16 ? 1 : rows <= 32 || d.head_dim > 64 ? 2 : 4;
+  s.R = rows <= 16 ? 1 : 2;
   s.RB = (int)((rows + 16 * s.R - 1) / (16 * s.R));
   const int64_t units = B * d.heads * s.RB;
   auto up = [](int64_t x) { return (x + 127) / 128 * 128; };
@@ -780,8 +836,7 @@ void launch_attend(const KvAttend& a, const KvSplit& s, hipStream_t stream) {
   const int64_t u = (int64_t)a.table.B * a.dims.heads * s.parts;
   const dim3 grid((unsigned)((u + 7) / 8 * 8 * s.RB)), block(256);
   if (s.R == 1) k_kv_attend<D, BITS, 1><<<grid, block, 0, stream>>>(a, s);
-  else if (s.R == 2) k_kv_attend<D, BITS, 2><<<grid, block, 0, stream>>>(a, s);
-  else if constexpr (D <= 64) k_kv_attend<D, BITS, 4><<<grid, block, 0, stream>>>(a, s);
+  else k_kv_attend<D, BITS, 2><<<grid, block, 0, stream>>>(a, s);
   if (s.parts <= 1) return;
   const int64_t x = (int64_t)a.T * a.q_heads;
   if (s.parts <= 8) k_kv_join<D, 1><<<(unsigned)((x + 3) / 4), 256, 0, stream>>>(a, s);
