@@ -172,6 +172,10 @@ __global__ __launch_bounds__(256) void k_kv_copy(KvCopy c, int tw) {
 // 2^8 (fp16 has room) or an exponential nears fp32's end.  So a weight is off
 // by at most half a step of fp16 whatever the range of the V scales, down to
 // s_v = 2^-60 of the row's largest exp2(s - r), and rescaling is rare.
+// Half a step of fp16 in each weight is an eighth of a bf16 output's own, but
+// as much as an fp16 output's: for those (FINE) a second product takes what
+// the rounding left (without it, their error against 64 bits was 1.4 to 1.5
+// times that of rounding the exact output).
 typedef _Float16 h2 __attribute__((ext_vector_type(2)));
 typedef _Float16 h8 __attribute__((ext_vector_type(8)));
 typedef float f4 __attribute__((ext_vector_type(4)));
@@ -525,12 +529,13 @@ struct KvLds {
 };
 
 // Waves a SIMD, by the registers that a row tile's outputs take.
-constexpr int kv_waves(int D, int BITS, int R) {
-  return D * R <= 64 || (D == 128 && R == 1 && BITS == 4) ? 4 : D * R <= 128 || (D == 128 && BITS == 4) ? 3 : 2;
+constexpr int kv_waves(int D, int BITS, int R, bool FINE) {
+  return D * R <= 64 || (D == 128 && R == 1 && BITS == 4) ? 4
+         : D * R <= 128 || (D == 128 && BITS == 4 && !FINE) ? 3 : 2;
 }
 
-template <int D, int BITS, int R>
-__global__ __launch_bounds__(256, kv_waves(D, BITS, R)) void k_kv_attend(KvAttend a, KvSplit sp) {
+template <int D, int BITS, int R, bool FINE>
+__global__ __launch_bounds__(256, kv_waves(D, BITS, R, FINE)) void k_kv_attend(KvAttend a, KvSplit sp) {
   constexpr int RB = D * BITS / 8;   // bytes of a cache row
   constexpr int KB = RB / 4, VB = RB / 16;
   constexpr int NK = D / 32;         // products over d
@@ -626,7 +631,7 @@ __global__ __launch_bounds__(256, kv_waves(D, BITS, R)) void k_kv_attend(KvAtten
       const uint32_t valid = __builtin_amdgcn_readfirstlane(L.p.valid[st]);
       const int64_t j0 = (int64_t)p0 + st * 32 - base;
       const bool whole = valid == ~0u && j0 <= -32;
-      h8 P[R];
+      h8 P[R], fine[FINE ? R : 1];
 #pragma unroll
       for (int rt = 0; rt < R; ++rt) {
         if constexpr (R > 1) __builtin_amdgcn_sched_barrier(0);
@@ -656,7 +661,10 @@ __global__ __launch_bounds__(256, kv_waves(D, BITS, R)) void k_kv_attend(KvAtten
           for (int j = 0; j < DB; ++j) O[rt][j] *= f;
         });
 #pragma unroll
-        for (int e = 0; e < 8; ++e) P[rt][e] = (_Float16)s[e];
+        for (int e = 0; e < 8; ++e) {
+          P[rt][e] = (_Float16)s[e];
+          if constexpr (FINE) fine[rt][e] = (_Float16)(s[e] - (float)P[rt][e]);
+        }
       }
 
       // O^T += V^T P^T, one element of d per lane column at a time
@@ -667,8 +675,10 @@ __global__ __launch_bounds__(256, kv_waves(D, BITS, R)) void k_kv_attend(KvAtten
       for (int j = 0; j < DB; ++j) {
         const h8 x = v_operand<VB, BITS>(vr, j);
 #pragma unroll
-        for (int rt = 0; rt < R; ++rt)
+        for (int rt = 0; rt < R; ++rt) {
           O[rt][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(x, P[rt], O[rt][j], 0, 0, 0);
+          if constexpr (FINE) O[rt][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(x, fine[rt], O[rt][j], 0, 0, 0);
+        }
       }
       if (more) load_v(st + 4);
     }
@@ -835,8 +845,13 @@ template <int D, int BITS>
 void launch_attend(const KvAttend& a, const KvSplit& s, hipStream_t stream) {
   const int64_t u = (int64_t)a.table.B * a.dims.heads * s.parts;
   const dim3 grid((unsigned)((u + 7) / 8 * 8 * s.RB)), block(256);
-  if (s.R == 1) k_kv_attend<D, BITS, 1><<<grid, block, 0, stream>>>(a, s);
-  else k_kv_attend<D, BITS, 2><<<grid, block, 0, stream>>>(a, s);
+  if (a.type == SONIQ_F16) {
+    if (s.R == 1) k_kv_attend<D, BITS, 1, true><<<grid, block, 0, stream>>>(a, s);
+    else k_kv_attend<D, BITS, 2, true><<<grid, block, 0, stream>>>(a, s);
+  } else {
+    if (s.R == 1) k_kv_attend<D, BITS, 1, false><<<grid, block, 0, stream>>>(a, s);
+    else k_kv_attend<D, BITS, 2, false><<<grid, block, 0, stream>>>(a, s);
+  }
   if (s.parts <= 1) return;
   const int64_t x = (int64_t)a.T * a.q_heads;
   if (s.parts <= 8) k_kv_join<D, 1><<<(unsigned)((x + 3) / 4), 256, 0, stream>>>(a, s);
