@@ -25,8 +25,9 @@ def quantize_rows(x, top=127.0):
 def i8_gemm(qa, sa, qw, sw, bias=None):
     """float32 outputs before their rounding to the output type: the fixed
     order (float(acc) * s_a) * s_w + bias."""
-    acc = qa.astype(np.int64) @ qw.astype(np.int64).T
+    acc = qa.astype(np.float64) @ qw.astype(np.float64).T   # sums of integers below 2^53: exact
     assert np.abs(acc).max(initial=0) < 2**31
+    acc = acc.astype(np.int32)
     with np.errstate(all="ignore"):
         y = (acc.astype(F32) * sa[:, None].astype(F32)).astype(F32)
         y = (y * sw[None, :].astype(F32)).astype(F32)

@@ -86,7 +86,7 @@ SHAPES = [  # M, N, K
     (128, 128, 4096), (129, 257, 385), (200, 2304, 768), (256, 256, 256), (257, 511, 1000), (301, 199, 4091),
     (513, 1025, 129), (1000, 300, 2048), (2049, 140, 320), (1, 70000, 64), (4097, 65, 64), (512, 2560, 1152),
     (130, 1300, 2065), (100, 10000, 2049), (70, 19300, 130), (2050, 1300, 100), (300, 9000, 1000), (3900, 4100, 200),
-    (66, 64, 1025), (64, 9999, 16), (200, 64, 15), (90, 30, 2000), (8200, 260, 16)]
+    (4090, 4085, 300), (4096, 4096, 16), (66, 64, 1025), (64, 9999, 16), (200, 64, 15), (90, 30, 2000), (8200, 260, 16)]
 
 
 @pytest.mark.parametrize("M,N,K", SHAPES, ids=lambda v: str(v))
@@ -146,6 +146,75 @@ def test_a_bad_token_spoils_itself_alone(M):
     bad[0] = bad[M // 2] = True
     assert bool(torch.isnan(Y[bad].float()).all())
     assert torch.equal(Y[~bad], ref[~bad])
+
+
+@pytest.mark.parametrize("M,N", [(65, 300), (3, 40), (300, 70)])
+def test_rows_far_apart(M, N):
+    """Row strides past 2^24 bytes, and tokens more than 4 GiB from the first."""
+    ld = (1 << 24) + 48
+    r = np.random.default_rng(7)
+    a = r.integers(-128, 128, (M, 200)).astype(np.int8)
+    big = torch.empty((M, ld), dtype=torch.int8, device="cuda")
+    A = big[:, 8:208]
+    A.copy_(torch.from_numpy(a))
+    W, w = _codes(N, 200, 8)
+    sa, sw = torch.rand(M, device="cuda"), torch.rand(N, device="cuda") / 1000
+    want = torch.from_numpy(serve.i8_gemm(a, sa.cpu().numpy(), w, sw.cpu().numpy()))
+    _same(sq.soniq_i8_gemm(A, sa, W, sw, dtype=torch.float32), want)
+    if M > 64:                                       # and as the weights
+        _same(sq.soniq_i8_gemm(W, sw, A, sa, dtype=torch.float32),
+              torch.from_numpy(serve.i8_gemm(w, sw.cpu().numpy(), a, sa.cpu().numpy())))
+
+
+def test_two_graphs_share_a_workspace():
+    """Two captured layers on one workspace, replayed in turn with eager calls
+    on it between them."""
+    W, _ = _codes(600, 512, 5)
+    sw = torch.rand(600, device="cuda") / 100
+    work = torch.empty(sq.soniq_quantize_i8_gemm_workspace(300, 512), dtype=torch.uint8, device="cuda")
+    xs = [_tokens(300, 512, "bf16", seed=1), _tokens(20, 512, "bf16", seed=2)]
+    want = [sq.soniq_quantize_i8_gemm(x, W, sw) for x in xs]
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    graphs, outs = [], []
+    for x in xs:
+        with torch.cuda.stream(side):
+            sq.soniq_quantize_i8_gemm(x, W, sw, work=work)
+        torch.cuda.synchronize()
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g, stream=side):
+            outs.append(sq.soniq_quantize_i8_gemm(x, W, sw, work=work))
+        graphs.append(g)
+    for k in (0, 1, 1, 0, 0, 1):
+        outs[k].zero_()
+        graphs[k].replay()
+        torch.cuda.synchronize()
+        assert torch.equal(outs[k], want[k])
+        assert torch.equal(sq.soniq_quantize_i8_gemm(xs[1 - k], W, sw, work=work), want[1 - k])
+        torch.cuda.synchronize()
+
+
+def test_binding_refusals():
+    """What the binding refuses before the library sees it."""
+    x = torch.randn((4, 64), device="cuda")
+    W, _ = _codes(20, 64, 5)
+    sw = torch.rand(20, device="cuda")
+    bad = [(TypeError, lambda: sq.soniq_quantize_rows(x.t())), (TypeError, lambda: sq.soniq_quantize_rows(x.double())),
+           (TypeError, lambda: sq.soniq_quantize_rows(x[:1].expand(4, 64))), (TypeError, lambda: sq.soniq_quantize_rows(x[0])),
+           (ValueError, lambda: sq.soniq_quantize_rows(x, scales=torch.empty(3, device="cuda"))),
+           (TypeError, lambda: sq.soniq_quantize_rows(x, out=torch.empty((4, 64), device="cuda"))),
+           (ValueError, lambda: sq.soniq_quantize_i8_gemm(x[:, :32], W, sw)),
+           (TypeError, lambda: sq.soniq_quantize_i8_gemm(x, W.float(), sw)),
+           (ValueError, lambda: sq.soniq_quantize_i8_gemm(x, W, sw[:3])),
+           (TypeError, lambda: sq.soniq_quantize_i8_gemm(x, W, sw.cpu())),
+           (TypeError, lambda: sq.soniq_quantize_i8_gemm(x, W, sw, dtype=torch.float64)),
+           (ValueError, lambda: sq.soniq_quantize_i8_gemm(x, W, sw, out=torch.empty((4, 21), device="cuda"))),
+           (sq.SoniqError, lambda: sq.soniq_quantize_i8_gemm(torch.randn((9, 64), device="cuda"), W, sw,
+                                                             work=torch.empty(16, dtype=torch.uint8, device="cuda"))),
+           (TypeError, lambda: sq.soniq_i8_gemm(x, sw, W, sw))]
+    for error, call in bad:
+        with pytest.raises(error):
+            call()
 
 
 def test_no_tokens():

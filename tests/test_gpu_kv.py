@@ -341,6 +341,48 @@ def test_long_cache_passes_32_bits():
     assert torch.equal(a, b)
 
 
+def test_binding_refusals():
+    cache = sq.KVCache.empty(4, 16, 2, 64)
+    t, cu, ln = _i32([[0, 1]]), _i32([0, 3]), _i32([20])
+    q = torch.zeros((3, 4, 64), dtype=torch.bfloat16, device="cuda")
+    k = torch.zeros((3, 2, 64), device="cuda")
+    att = lambda **kw: sq.soniq_kv_attention(cache, kw.pop("q", q), kw.pop("t", t), kw.pop("cu", cu), kw.pop("ln", ln), **kw)
+    bad = [(TypeError, lambda: att(t=t.long())), (ValueError, lambda: att(cu=cu[:1])), (TypeError, lambda: att(ln=ln.cpu())),
+           (sq.SoniqError, lambda: att(q=q.float())), (TypeError, lambda: att(q=q.double())),
+           (sq.SoniqError, lambda: att(q=q[:, :3])), (ValueError, lambda: att(q=q[..., :32])),
+           (ValueError, lambda: att(q=q.transpose(1, 2).contiguous().transpose(1, 2))),
+           (TypeError, lambda: att(mask=torch.zeros((3, 1), dtype=torch.int32, device="cuda"))),
+           (ValueError, lambda: att(mask=torch.zeros((2, 1), dtype=torch.int64, device="cuda"))),
+           (sq.SoniqError, lambda: att(mask=torch.zeros((3, 5), dtype=torch.int64, device="cuda"))),
+           (sq.SoniqError, lambda: att(max_q=257)), (ValueError, lambda: att(out=q.half())),
+           (TypeError, lambda: att(out=torch.empty_like(q[:1]).expand(3, 4, 64))),
+           (ValueError, lambda: att(lse=torch.zeros((3, 3), device="cuda"))),
+           (ValueError, lambda: sq.soniq_kv_write(cache, k, k[..., ::2], t, cu, ln)),
+           (ValueError, lambda: sq.soniq_kv_write(cache, torch.zeros((3, 2, 128), device="cuda")[..., ::2], k, t, cu, ln)),
+           (ValueError, lambda: sq.soniq_kv_write(cache, k.half(), k, t, cu, ln)),
+           (ValueError, lambda: sq.soniq_kv_write(cache, k[:, :1], k[:, :1], t, cu, ln)),
+           (ValueError, lambda: sq.soniq_kv_read(cache, t, cu, ln, 4, out=(k, k))),
+           (ValueError, lambda: sq.KVCache.empty(4, 16, 2, 64, bits=2)), (TypeError, lambda: sq.KVCache(k, k, k, k)),
+           (ValueError, lambda: sq.KVCache(cache.k, cache.k_scale, cache.v[:1], cache.v_scale))]
+    for i, (error, call) in enumerate(bad):
+        with pytest.raises(error):
+            call()
+            print("not refused:", i)
+
+
+def test_no_sequences_and_no_tokens():
+    cache = sq.KVCache.empty(4, 16, 2, 64)
+    none = torch.empty((0, 2), dtype=torch.int32, device="cuda")
+    q = torch.full((3, 4, 64), 2.0, dtype=torch.bfloat16, device="cuda")
+    out = torch.full_like(q, 7.0)
+    sq.soniq_kv_attention(cache, q, none, _i32([0]), _i32([]), out=out)
+    assert bool((out == 7.0).all())
+    assert sq.soniq_kv_attention(cache, q[:0], _i32([[0]]), _i32([0, 0]), _i32([5])).shape == (0, 4, 64)
+    k = torch.zeros((0, 2, 64), device="cuda")
+    sq.soniq_kv_write(cache, k, k, _i32([[0]]), _i32([0, 0]), _i32([0]))
+    assert sq.soniq_kv_read(cache, _i32([[0]]), _i32([0, 0]), _i32([0]), 0)[0].shape == (0, 2, 64)
+
+
 # ------------------------------------------------------------ used together --
 def _layer(r, hidden, heads, group, D):
     W = {"qkv": ((group + 2) * heads * D, hidden), "out": (hidden, group * heads * D)}
