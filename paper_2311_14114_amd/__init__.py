@@ -540,6 +540,16 @@ def _raw_stream(stream, device: int):
     return torch._C._cuda_getCurrentRawStream(device)
 
 
+def _empty(shape, dtype, device, stream):
+    """Memory that a call on `stream` writes: taken on that stream, so that it
+    is neither in use elsewhere before nor given away too early after."""
+    if stream is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    s = torch.cuda.ExternalStream(int(stream), device) if int(stream) else torch.cuda.default_stream(device)
+    with torch.cuda.stream(s):
+        return torch.empty(shape, dtype=dtype, device=device)
+
+
 def _refuse(t, what: str, d: int, dtype, dim: int):
     if not isinstance(t, torch.Tensor) or not t.is_cuda:
         raise TypeError(f"{what} must be a device tensor")
@@ -598,26 +608,26 @@ def soniq_quantize_rows(A, out=None, scales=None, stream=None):
     M, K = A.shape
     lda = _ld(A, "A", M, K)
     if out is None:
-        out = torch.empty((M, -(-K // 16) * 16), dtype=torch.int8, device=A.device)[:, :K]
+        out = _empty((M, -(-K // 16) * 16), torch.int8, A.device, stream)[:, :K]
     else:
         _is(out, "out", d, torch.int8, 2)
         if out.shape != A.shape:
             raise ValueError("out must have A's shape")
     if scales is None:
-        scales = torch.empty(M, dtype=torch.float32, device=A.device)
+        scales = _empty(M, torch.float32, A.device, stream)
     s = _vector(scales, "scales", d, torch.float32, M)
     _check(_lib.soniq_quantize_rows(A.data_ptr(), ta, M, K, lda, out.data_ptr(), _ld(out, "out", M, K), s,
                                      _raw_stream(stream, d)))
     return out, scales
 
 
-def _i8_operands(W, s_w, bias, d, M, K, out, dtype, device):
+def _i8_operands(W, s_w, bias, d, M, K, out, dtype, device, stream):
     _is(W, "W", d, torch.int8, 2)
     N, Kw = W.shape
     if Kw != K:
         raise ValueError("W has the wrong number of input channels")
     if out is None:
-        out = torch.empty((M, N), dtype=torch.bfloat16 if dtype is None else dtype, device=device)
+        out = _empty((M, N), torch.bfloat16 if dtype is None else dtype, device, stream)
     else:
         _is(out, "out", d, out.dtype if dtype is None else dtype, 2)
         if out.shape[0] != M or out.shape[1] != N:
@@ -634,7 +644,7 @@ def soniq_i8_gemm(A, s_a, W, s_w, bias=None, out=None, dtype=None, stream=None):
     _is(A, "A", d, torch.int8, 2)
     M, K = A.shape
     sa = _vector(s_a, "s_a", d, torch.float32, M)
-    N, w, ldw, sw, b, out = _i8_operands(W, s_w, bias, d, M, K, out, dtype, A.device)
+    N, w, ldw, sw, b, out = _i8_operands(W, s_w, bias, d, M, K, out, dtype, A.device, stream)
     _check(_lib.soniq_i8_gemm(A.data_ptr(), _ld(A, "A", M, K), sa, w, ldw, sw, b, M, N, K, out.data_ptr(),
                                _type_of(out, "out"), _ld(out, "out", M, N), _raw_stream(stream, d)))
     return out
@@ -647,11 +657,11 @@ def soniq_quantize_i8_gemm_workspace(M: int, K: int) -> int:
     return n.value
 
 
-def _work(work, need: int, d: int, device):
+def _work(work, need: int, d: int, device, stream):
     if work is None:
         if need == 0:
             return None, 0, None
-        work = torch.empty(need, dtype=torch.uint8, device=device)
+        work = _empty(need, torch.uint8, device, stream)
         return work.data_ptr(), need, work
     _is(work, "work", d, torch.uint8, 1)
     if not work.is_contiguous():
@@ -668,8 +678,8 @@ def soniq_quantize_i8_gemm(A, W, s_w, bias=None, out=None, dtype=None, work=None
     _is(A, "A", d, A.dtype, 2)
     M, K = A.shape
     lda = _ld(A, "A", M, K)
-    N, w, ldw, sw, b, out = _i8_operands(W, s_w, bias, d, M, K, out, dtype, A.device)
-    wp, wn, work = _work(work, soniq_quantize_i8_gemm_workspace(M, K), d, A.device)
+    N, w, ldw, sw, b, out = _i8_operands(W, s_w, bias, d, M, K, out, dtype, A.device, stream)
+    wp, wn, work = _work(work, soniq_quantize_i8_gemm_workspace(M, K), d, A.device, stream)
     _check(_lib.soniq_quantize_i8_gemm(A.data_ptr(), ta, lda, w, ldw, sw, b, M, N, K, out.data_ptr(),
                                         _type_of(out, "out"), _ld(out, "out", M, N), wp, wn,
                                         _raw_stream(stream, d)))
@@ -775,7 +785,7 @@ def soniq_kv_read(cache: KVCache, page_table, cu, start, tokens: int, dtype=None
     heads, D = cache.heads, cache.head_dim
     if out is None:
         dtype = torch.bfloat16 if dtype is None else dtype
-        K, V = torch.empty((2, tokens, heads, D), dtype=dtype, device=cache.device).unbind(0)
+        K, V = _empty((2, tokens, heads, D), dtype, cache.device, stream).unbind(0)
         tk, kts, khs = _type_of(K, "dtype:"), heads * D, D
         vts, vhs = kts, khs
     else:
@@ -827,7 +837,7 @@ def soniq_kv_attention(cache: KVCache, q, page_table, cu, kv_len, scale=None, ma
     if D != cache.head_dim or unit != 1:
         raise ValueError(f"q must be [T, q_heads, {cache.head_dim}] with unit stride in its last dimension")
     if out is None:
-        out = torch.empty((T, heads, D), dtype=q.dtype, device=cache.device)
+        out = _empty((T, heads, D), q.dtype, cache.device, stream)
         ots, ohs = heads * D, D
     else:
         to, ots, ohs = _kv_rows(out, "out", d, heads, D)
@@ -848,7 +858,7 @@ def soniq_kv_attention(cache: KVCache, q, page_table, cu, kv_len, scale=None, ma
         max_q = max(T, 1)
     if max_kv is None:
         max_kv = width * cache.page_size
-    wp, wn, work = _work(work, soniq_kv_attention_workspace(cache, T, heads, B, max_q, max_kv), d, cache.device)
+    wp, wn, work = _work(work, soniq_kv_attention_workspace(cache, T, heads, B, max_q, max_kv), d, cache.device, stream)
     _check(_lib.soniq_kv_attention(cache._ref, q.data_ptr(), qts, qhs, code, T, heads, table, ld, width, B, cu,
                                     kv_len, bits, words, D ** -0.5 if scale is None else scale, max_q, max_kv,
                                     out.data_ptr(), ots, ohs, None if lse is None else lse.data_ptr(), wp, wn,

@@ -194,6 +194,28 @@ def test_two_graphs_share_a_workspace():
         torch.cuda.synchronize()
 
 
+def test_a_given_stream_owns_what_the_call_allocates():
+    """The current stream gets none of the memory that a call on another one
+    still uses: its workspace, freed as the call returns, stays that stream's."""
+    W, _ = _codes(256, 512, 5)
+    sw = torch.rand(256, device="cuda") / 100
+    x = _tokens(4096, 512, "bf16", seed=3)
+    want = sq.soniq_quantize_i8_gemm(x, W, sw)
+    need = sq.soniq_quantize_i8_gemm_workspace(4096, 512)
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    torch.cuda.empty_cache()
+    with torch.cuda.stream(side):
+        torch.cuda._sleep(50_000_000)                # the call waits behind this
+    got = sq.soniq_quantize_i8_gemm(x, W, sw, stream=side.cuda_stream)
+    mine = torch.full((need,), 77, dtype=torch.uint8, device="cuda")
+    torch.cuda.synchronize()
+    assert bool((mine == 77).all())
+    assert torch.equal(got, want)
+    q, s = sq.soniq_quantize_rows(x, stream=torch.cuda.default_stream().cuda_stream)
+    assert torch.equal(sq.soniq_i8_gemm(q, s, W, sw, stream=0), want)
+
+
 def test_binding_refusals():
     """What the binding refuses before the library sees it."""
     x = torch.randn((4, 64), device="cuda")
