@@ -540,7 +540,8 @@ soniq_status soniq_quantize_rows(const void* A_dev, int a_type, int64_t M, int64
  *   bias_dev device, fp32 [N], or NULL
  *   Y_dev    device, y_type [M, ldy]; columns N.. of a row are not written
  * M = 0 is allowed and does nothing.  Errors: INVALID_ARGUMENT, UNSUPPORTED
- * (K > SONIQ_MAX_K, M >= 2^31, N >= 2^26, or M * N / 4096 >= 2^24), HIP.
+ * (K > SONIQ_MAX_K, M >= 2^31, N >= 2^26, or M * N / 4096 >= 2^24 - 8 with M
+ * and N rounded up to multiples of 64), HIP.
  */
 soniq_status soniq_i8_gemm(const int8_t* A_dev, int64_t lda, const float* s_a_dev,
                            const int8_t* W_dev, int64_t ldw, const float* s_w_dev,
@@ -646,6 +647,7 @@ soniq_status soniq_kv_read(const soniq_kv_cache_t* cache, void* K_dev, int64_t k
  *   kv_len_dev device, int32 [B]
  *   mask_dev   device, uint64 [T, mask_words], or NULL (mask_words then 0);
  *              tokens past the mask's 64 * mask_words bits are not seen
+ *   scale      finite, of either sign
  *   max_q      the largest n, at most 256; queries of a sequence from max_q
  *              on are not computed (their rows are left as they were)
  *   max_kv     the largest kv_len; only a hint for the split of the work,

@@ -1,5 +1,6 @@
 // Host side of the 8-bit linear layers and the quantized key/value cache:
 // argument checks, workspaces, dispatch.
+#include <cmath>
 #include <cstdarg>
 #include <cstdint>
 
@@ -38,7 +39,7 @@ soniq_status fail(soniq_status st, const char* fmt, ...) {
   } while (0)
 
 constexpr int64_t kMax31 = (int64_t)1 << 31;
-constexpr int64_t kMaxGroups = (int64_t)1 << 24;  // workgroups of 256 threads in a launch
+constexpr int64_t kMaxGroups = (int64_t)1 << 24;  // workgroups of 256 threads in a launch: 2^32 threads are too many
 
 int type_size(int type) { return type == SONIQ_F32 ? 4 : type == SONIQ_BF16 || type == SONIQ_F16 ? 2 : 0; }
 
@@ -71,8 +72,8 @@ soniq_status check_gemm(const char* who, const void* W, int64_t ldw, const float
   NEED(W && s_w && (Y || M == 0), "%s: null pointer", who);
   NEED(aligned(s_w, 4) && aligned(bias, 4) && aligned(Y, type_size(y_type)),
        "%s: s_w, bias or Y is not aligned to its elements", who);
-  LIMIT(K <= SONIQ_MAX_K && M < kMax31 && N < kMax31 / 32 && ((M + 63) / 64) * ((N + 63) / 64) < kMaxGroups,
-        "%s: M = %lld, N = %lld, K = %lld (M < 2^31, N < 2^26, M * N / 4096 < 2^24, K <= %d)", who,
+  LIMIT(K <= SONIQ_MAX_K && M < kMax31 && N < kMax31 / 32 && ((M + 63) / 64) * ((N + 63) / 64) < kMaxGroups - 8,
+        "%s: M = %lld, N = %lld, K = %lld (M < 2^31, N < 2^26, M * N / 4096 < 2^24 - 8, K <= %d)", who,
         (long long)M, (long long)N, (long long)K, SONIQ_MAX_K);
   return SONIQ_OK;
 }
@@ -271,6 +272,7 @@ soniq_status soniq_kv_attention(const soniq_kv_cache_t* cache, const void* q_dev
   NEED(type == SONIQ_BF16 || type == SONIQ_F16, "%s: type %d is not SONIQ_BF16 or SONIQ_F16", who, type);
   NEED(mask_dev ? mask_words >= 1 && mask_words <= 4 : mask_words == 0,
        "%s: %d mask words (1 to 4 with a mask, 0 without)", who, mask_words);
+  NEED(std::isfinite(scale), "%s: the scale is not finite", who);
   if (T == 0 || B == 0) return SONIQ_OK;
   NEED(q_dev && out_dev, "%s: null q or out", who);
   NEED(aligned(q_dev, 2) && aligned(out_dev, 2) && aligned(mask_dev, 8) && aligned(lse_dev, 4),

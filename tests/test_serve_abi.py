@@ -49,6 +49,7 @@ BOTH = dict(A=FAKE, type=0, lda=32, W=FAKE, ldw=32, s_w=FAKE, bias=None, M=6, N=
     ("gemm", GEMM, dict(K=0), BAD), ("gemm", GEMM, dict(M=-1), BAD), ("gemm", GEMM, dict(y_type=5), BAD),
     ("gemm", GEMM, dict(Y=FAKE + 1), BAD), ("gemm", GEMM, dict(bias=FAKE + 1), BAD),
     ("gemm", GEMM, dict(K=70000, lda=70000, ldw=70000), UNSUP), ("gemm", GEMM, dict(N=1 << 31, ldy=1 << 31), UNSUP),
+    ("gemm", GEMM, dict(M=(1 << 30) - 64), UNSUP), ("gemm", GEMM, dict(M=1 << 16, N=1 << 20, ldy=1 << 20), UNSUP),
     ("both", BOTH, dict(A=None), BAD), ("both", BOTH, dict(W=None), BAD), ("both", BOTH, dict(work=None), BAD),
     ("both", BOTH, dict(work=FAKE + 8), BAD), ("both", BOTH, dict(bytes=6 * 32 + 23), BAD),
     ("both", BOTH, dict(lda=31), BAD), ("both", BOTH, dict(y_type=9), BAD)],
@@ -90,7 +91,8 @@ def test_copy_refusals(L, fn, changes, status):
     (dict(kv_len=None), BAD), (dict(q=None), BAD), (dict(out=None), BAD), (dict(type=0), BAD), (dict(heads=3), BAD),
     (dict(heads=0), BAD), (dict(max_q=0), BAD), (dict(max_kv=-1), BAD), (dict(max_q=257), UNSUP),
     (dict(mask=FAKE), BAD), (dict(words=1), BAD), (dict(mask=FAKE, words=5), BAD), (dict(mask=FAKE + 4, words=1), BAD),
-    (dict(work=FAKE + 8), BAD), (dict(lse=FAKE + 2), BAD)], ids=str)
+    (dict(work=FAKE + 8), BAD), (dict(lse=FAKE + 2), BAD), (dict(scale=float("nan")), BAD),
+    (dict(scale=float("inf")), BAD)], ids=str)
 def test_attention_refusals(L, changes, status):
     c = _cache()
     assert L.soniq_kv_attention(*_with(ATTEND, cache=ctypes.addressof(c), **changes)) == status
