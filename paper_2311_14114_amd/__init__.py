@@ -710,6 +710,8 @@ class KVCache:
             raise ValueError("k, v and the scales have different extents")
         self.k, self.k_scale, self.v, self.v_scale, self.bits = k, k_scale, v, v_scale, bits
         self.pages, self.heads, self.page_size, width = k.shape
+        if self.pages * self.heads * self.page_size >= 1 << 31:
+            raise ValueError("a cache has fewer than 2^31 rows")
         self.head_dim = width * 8 // bits
         self.device, self.device_index = k.device, d
         self._c = KVCacheStruct(k.data_ptr(), k_scale.data_ptr(), v.data_ptr(), v_scale.data_ptr(),
@@ -757,7 +759,8 @@ def _kv_rows(t, what: str, d: int, heads: int, head_dim: int):
 def _kv_out(t, what: str, ts: int, hs: int):
     """An output's rows must not overlap."""
     T, heads, n = t.shape
-    if (T > 1 and ts < n) or (heads > 1 and hs < n):
+    (a, na), (b, nb) = sorted(((ts, T), (hs, heads)))
+    if T * heads and ((na > 1 and a < n) or (nb > 1 and b < (a * (na - 1) if na > 1 else 0) + n)):
         raise TypeError(f"{what} has rows that overlap")
 
 

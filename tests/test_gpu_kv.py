@@ -193,6 +193,97 @@ def test_the_hint_changes_nothing_but_rounding(max_kv):
     _check_attention(cache, h, q, table, [0, 1, 2], lens, 8, max_kv=max_kv)
 
 
+@pytest.mark.parametrize("bits", [8, 4])
+@pytest.mark.parametrize("dtype", ["bf16", "fp16"])
+def test_head_major_operands_and_shared_pages(dtype, bits):
+    """[heads, tokens, head_dim] operands, a table that is a slice of a wider
+    one, a prefix that two sequences share, a page that one holds twice."""
+    r = np.random.default_rng(21)
+    page, heads, group, D, B = 16, 2, 4, 128, 3
+    wide = np.full((B, 40), 5, np.int32)
+    cache, h = _random_cache(r, 30, page, heads, D, bits)
+    wide[0, 3:9] = [4, 7, 9, 11, 4, 13]               # page 4 twice
+    wide[1, 3:9] = [4, 7, 9, 15, 16, 17]              # the first three shared with sequence 0
+    wide[2, 3:9] = [20, 21, 22, 23, 24, -1]
+    table = torch.from_numpy(wide).cuda()[:, 3:9]
+    start, new = [90, 70, 61], [3, 5, 2]
+    cu = [0, 3, 8, 10]
+    kv = torch.randn((2, heads, 11, D), device="cuda").to(TYPES[dtype])
+    K, V = kv[0].transpose(0, 1), kv[1].transpose(0, 1)
+    sq.soniq_kv_write(cache, K, V, table, _i32(cu), _i32(start))
+    narrow = np.ascontiguousarray(wide[:, 3:9])
+    serve.kv_write(h["k"], h["ks"], K.float().cpu().numpy(), narrow, cu, start, bits)
+    serve.kv_write(h["v"], h["vs"], V.float().cpu().numpy(), narrow, cu, start, bits)
+    np.testing.assert_array_equal(cache.k.cpu().numpy().view(np.uint8), h["k"])
+    np.testing.assert_array_equal(cache.v_scale.cpu().numpy(), h["vs"])
+    back = torch.full((2, heads, 11, D), 3.0, dtype=TYPES[dtype], device="cuda")
+    sq.soniq_kv_read(cache, table, _i32(cu), _i32(start), 11, out=(back[0].transpose(0, 1), back[1].transpose(0, 1)))
+    k, v = sq.soniq_kv_read(cache, table, _i32(cu), _i32(start), 11, dtype=TYPES[dtype])
+    assert torch.equal(back[0].transpose(0, 1)[:10], k[:10]) and torch.equal(back[1].transpose(0, 1)[:10], v[:10])
+    assert bool((back[:, :, 10] == 3.0).all())
+    lens = [a + n for a, n in zip(start, new)]
+    q = torch.randn((heads * group, 11, D), device="cuda").to(TYPES[dtype]).transpose(0, 1)
+    want = _check_attention(cache, h, q, narrow, cu, lens, bits)
+    out = torch.full((heads * group, 11, D), 3.0, dtype=TYPES[dtype], device="cuda")
+    work = torch.empty(sq.soniq_kv_attention_workspace(cache, 11, heads * group, B, 8, 200) + 64, dtype=torch.uint8,
+                       device="cuda")
+    sq.soniq_kv_attention(cache, q, table, _i32(cu), _i32(lens), out=out.transpose(0, 1), work=work, max_q=8, max_kv=200)
+    far = (out.transpose(0, 1)[:10].float() - want[:10].float()).abs()
+    # Another split of the same sums.  Each result is off by half a step of its
+    # type and, for bf16, by half a step of the fp16 weights, 2^-11 of
+    # sum |w v| <= max |v| < 8: 2 (eps / 2 |o| + 2^-8) < 4 eps (1 + |o|).
+    assert bool((far <= 4 * torch.finfo(q.dtype).eps * (1 + want[:10].float().abs())).all())
+    assert bool((out[:, 10] == 3.0).all())
+
+
+@pytest.mark.parametrize("max_kv", [None, 60])
+def test_many_sequences(max_kv):
+    """More sequences than a wave has lanes, many of them without new tokens
+    or without positions, lengths on both sides of a part's."""
+    r = np.random.default_rng(22)
+    B = 200
+    new = r.choice([0, 1, 1, 2, 9], B).tolist()
+    lens = [int(n * r.integers(0, 2) + r.choice([0, 5, 130, 900, 2600])) for n in new]
+    pages, table = _tables(r, lens, 64)
+    cache, h = _random_cache(r, pages, 64, 1, 64, 8)
+    cu = np.concatenate(([0], np.cumsum(new))).tolist()
+    q = torch.from_numpy(r.standard_normal((sum(new) + 3, 2, 64)).astype(np.float32)).to(torch.bfloat16).cuda()
+    _check_attention(cache, h, q, table, cu, lens, 8, max_q=9, max_kv=max_kv)
+
+
+def test_two_graphs_share_a_workspace():
+    """Two layers' attention captured on one workspace, replayed in turn, with
+    eager work on it between the replays."""
+    r = np.random.default_rng(23)
+    lens = [3000, 41]
+    pages, table = _tables(r, lens, 16)
+    caches = [_random_cache(r, pages, 16, 2, 128, b)[0] for b in (8, 4)]
+    t, cu, ln = torch.from_numpy(table).cuda(), _i32([0, 2, 3]), _i32(lens)
+    qs = [torch.randn((3, 8, 128), device="cuda").to(torch.bfloat16) for _ in range(2)]
+    work = torch.empty(sq.soniq_kv_attention_workspace(caches[0], 3, 8, 2, 2, 3000), dtype=torch.uint8, device="cuda")
+    assert work.numel() > 0
+    call = lambda i: sq.soniq_kv_attention(caches[i], qs[i], t, cu, ln, max_q=2, max_kv=3000, work=work)
+    want = [call(0), call(1)]
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    graphs, outs = [], []
+    for i in range(2):
+        with torch.cuda.stream(side):
+            call(i)
+        torch.cuda.synchronize()
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g, stream=side):
+            outs.append(call(i))
+        graphs.append(g)
+    for k in (0, 1, 1, 0, 0, 1):
+        outs[k].zero_()
+        graphs[k].replay()
+        torch.cuda.synchronize()
+        assert torch.equal(outs[k], want[k])
+        assert torch.equal(call(1 - k), want[1 - k])
+        torch.cuda.synchronize()
+
+
 def test_rows_that_see_nothing():
     """No cached position, masks without a bit, lengths shorter than the new
     tokens: zeros and -inf, whatever the cache holds."""
@@ -356,18 +447,24 @@ def test_binding_refusals():
            (sq.SoniqError, lambda: att(mask=torch.zeros((3, 5), dtype=torch.int64, device="cuda"))),
            (sq.SoniqError, lambda: att(max_q=257)), (ValueError, lambda: att(out=q.half())),
            (TypeError, lambda: att(out=torch.empty_like(q[:1]).expand(3, 4, 64))),
+           (TypeError, lambda: att(out=torch.as_strided(torch.empty_like(q), (3, 4, 64), (64, 64, 1)))),
+           (TypeError, lambda: att(out=torch.as_strided(torch.empty_like(q), (3, 4, 64), (64, 128, 1)))),
+           (sq.SoniqError, lambda: att(scale=float("nan"))),
+           (sq.SoniqError, lambda: att(max_kv=5000, work=torch.empty(64, dtype=torch.uint8, device="cuda"))),
+           (sq.SoniqError, lambda: att(max_kv=5000, work=torch.empty(1 << 20, dtype=torch.uint8, device="cuda")[8:])),
+           (TypeError, lambda: att(work=torch.empty(1 << 20, dtype=torch.float32, device="cuda"))),
            (ValueError, lambda: att(lse=torch.zeros((3, 3), device="cuda"))),
            (ValueError, lambda: sq.soniq_kv_write(cache, k, k[..., ::2], t, cu, ln)),
-           (ValueError, lambda: sq.soniq_kv_write(cache, torch.zeros((3, 2, 128), device="cuda")[..., ::2], k, t, cu, ln)),
+           (TypeError, lambda: sq.soniq_kv_write(cache, torch.zeros((3, 2, 128), device="cuda")[..., ::2], k, t, cu, ln)),
            (ValueError, lambda: sq.soniq_kv_write(cache, k.half(), k, t, cu, ln)),
            (ValueError, lambda: sq.soniq_kv_write(cache, k[:, :1], k[:, :1], t, cu, ln)),
            (ValueError, lambda: sq.soniq_kv_read(cache, t, cu, ln, 4, out=(k, k))),
            (ValueError, lambda: sq.KVCache.empty(4, 16, 2, 64, bits=2)), (TypeError, lambda: sq.KVCache(k, k, k, k)),
            (ValueError, lambda: sq.KVCache(cache.k, cache.k_scale, cache.v[:1], cache.v_scale))]
     for i, (error, call) in enumerate(bad):
+        print("[gpu] refusal", i, flush=True)
         with pytest.raises(error):
             call()
-            print("not refused:", i)
 
 
 def test_no_sequences_and_no_tokens():
