@@ -162,7 +162,8 @@ __global__ __launch_bounds__(256) void k_kv_copy(KvCopy c, int tw) {
 // lost); V would lose digits over a long context, so one packed fma makes it
 // (u - zero) * 2^-9 first.
 // Queries are scaled by a power of two per row to use fp16's whole range
-// (bf16 queries are exact in it down to 2^-22 of the row's largest element).
+// (bf16 queries are exact in it down to 2^-22 of the row's largest element,
+// the sixteenths that meet odd 4-bit codes too).
 //
 // Softmax of a row over the positions so far, all in fp32 and base 2, has one
 // reference r for the sum and the weights:
@@ -255,16 +256,34 @@ __device__ __forceinline__ void softmax_step(float (&x)[N], const float (&v)[N],
   for (int e = 0; e < N; ++e) x[e] = w[e];
 }
 
+// Weights as fp16 and what that left of them.  Both are cut, not rounded: the
+// second takes up what the first cuts, and itself cuts less than 2^-20 of the
+// weight.
+__device__ __forceinline__ void weigh_fine(const float (&w)[8], h8& coarse, h8& fine) {
+  union { h2 p[4]; h8 v; } a, b;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    a.p[i] = __builtin_bit_cast(h2, __builtin_amdgcn_cvt_pkrtz(w[2 * i], w[2 * i + 1]));
+    float lo, hi;  // w - a, exact: one instruction from the fp16 half
+    asm("v_fma_mix_f32 %0, %1, -1.0, %2 op_sel_hi:[1,0,0]" : "=v"(lo) : "v"(a.p[i]), "v"(w[2 * i]));
+    asm("v_fma_mix_f32 %0, %1, -1.0, %2 op_sel:[1,0,0] op_sel_hi:[1,0,0]" : "=v"(hi) : "v"(a.p[i]), "v"(w[2 * i + 1]));
+    b.p[i] = __builtin_bit_cast(h2, __builtin_amdgcn_cvt_pkrtz(lo, hi));
+  }
+  coarse = a.v, fine = b.v;
+}
+
 // Two V codes moved to unsigned, times 2^-9.
-template <int BITS>
+// (UP: times 16 before that, as they lie in the odd nibbles.)
+template <int BITS, bool UP>
 __device__ __forceinline__ h2 v_half(uint32_t u16pair) {
   const h2 x = __builtin_bit_cast(h2, u16pair);
-  const _Float16 z = BITS == 8 ? (_Float16)-0.25f : (_Float16)-0x1p-6f;
-  return __builtin_elementwise_fma(x, h2{(_Float16)32768.0f, (_Float16)32768.0f}, h2{z, z});
+  const _Float16 z = BITS == 8 ? (_Float16)-0.25f : (_Float16)-0x1p-6f, m = UP ? (_Float16)2048.0f : (_Float16)32768.0f;
+  return __builtin_elementwise_fma(x, h2{m, m}, h2{z, z});
 }
 
 // Eight K codes as an operand: from two words of 8-bit codes in order, or
-// from one word of 4-bit codes in the order 0 4 1 5 2 6 3 7.
+// from one word of 4-bit codes in the order 0 4 1 5 2 6 3 7, the odd ones
+// times 16 (no shift; the queries hold a sixteenth there).
 template <int BITS>
 __device__ __forceinline__ h8 k_operand(const uint32_t* w) {
   union { uint32_t p[4]; h8 v; } r;
@@ -276,9 +295,12 @@ __device__ __forceinline__ h8 k_operand(const uint32_t* w) {
       r.p[2 * i + 1] = __builtin_amdgcn_perm(u, u, 0x0c030c02u);
     }
   } else {
-    const uint32_t u = w[0] ^ 0x88888888u;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) r.p[i] = (u >> (4 * i)) & 0x000F000Fu;
+    for (int i = 0; i < 2; ++i) {
+      const uint32_t u = w[0] >> (8 * i);
+      r.p[2 * i] = (u ^ 0x00080008u) & 0x000F000Fu;
+      r.p[2 * i + 1] = (u ^ 0x00800080u) & 0x00F000F0u;
+    }
   }
   return r.v;
 }
@@ -320,25 +342,26 @@ struct Raw {
   }
 };
 
-// A lane's V codes moved to unsigned, and from eight positions of them the
-// operand of its element j.
+// From a lane's V codes of eight positions the operand of its element j.
 template <int VB, int BITS>
 __device__ __forceinline__ void v_unsigned(Raw<VB>& r) {
+  if constexpr (BITS == 8) {
 #pragma unroll
-  for (int i = 0; i < (VB + 3) / 4; ++i) r.w[i] ^= BITS == 8 ? 0x80808080u : 0x88888888u;
+    for (int i = 0; i < (VB + 3) / 4; ++i) r.w[i] ^= 0x80808080u;
+  }
 }
-template <int VB, int BITS>
+template <int VB, int BITS, bool ODD>
 __device__ __forceinline__ h8 v_operand(const Raw<VB> (&r)[8], int j) {
   union { h2 p[4]; h8 v; } x;
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
     uint32_t lo = r[2 * i].w[j * BITS / 32], hi = r[2 * i + 1].w[j * BITS / 32];
     if constexpr (BITS == 4) {
-      lo = (lo >> (4 * (j & 1))) & 0x0F0F0F0Fu;
-      hi = (hi >> (4 * (j & 1))) & 0x0F0F0F0Fu;
+      lo = ODD ? (lo ^ 0x80808080u) & 0xF0F0F0F0u : (lo ^ 0x08080808u) & 0x0F0F0F0Fu;
+      hi = ODD ? (hi ^ 0x80808080u) & 0xF0F0F0F0u : (hi ^ 0x08080808u) & 0x0F0F0F0Fu;
     }
     const uint32_t by = j * BITS / 8 % 4;
-    x.p[i] = v_half<BITS>(__builtin_amdgcn_perm(hi, lo, 0x0c000c00u | (4 + by) << 16 | by));
+    x.p[i] = v_half<BITS, BITS == 4 && ODD>(__builtin_amdgcn_perm(hi, lo, 0x0c000c00u | (4 + by) << 16 | by));
   }
   return x.v;
 }
@@ -464,9 +487,11 @@ struct KvQuery {
       h8 v;
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
-        const _Float16 y = (_Float16)(value(8 * g + i) * down);
+        constexpr float kOdd = BITS == 4 ? 16.0f : 1.0f;  // as k_operand takes them
+        const float unit = i % 2 ? kOdd : 1.0f;
+        const _Float16 y = (_Float16)(value(8 * g + i) * (down * (1.0f / unit)));
         v[k_order<BITS>(i)] = y;
-        sum += (float)y;
+        sum += (float)y * unit;
       }
       const int d = d0 + 8 * g;
       q[r / 16][d % (D / 4) / 8][d / (D / 4) * 16 + r % 16] = v;
@@ -529,13 +554,13 @@ struct KvLds {
 };
 
 // Waves a SIMD, by the registers that a row tile's outputs take.
-constexpr int kv_waves(int D, int BITS, int R, bool FINE) {
+constexpr int kv_waves(int D, int BITS, int R) {
   return D * R <= 64 || (D == 128 && R == 1 && BITS == 4) ? 4
-         : D * R <= 128 || (D == 128 && BITS == 4 && !FINE) ? 3 : 2;
+         : D * R <= 128 || (D == 128 && BITS == 4) ? 3 : 2;
 }
 
 template <int D, int BITS, int R, bool FINE>
-__global__ __launch_bounds__(256, kv_waves(D, BITS, R, FINE)) void k_kv_attend(KvAttend a, KvSplit sp) {
+__global__ __launch_bounds__(256, kv_waves(D, BITS, R)) void k_kv_attend(KvAttend a, KvSplit sp) {
   constexpr int RB = D * BITS / 8;   // bytes of a cache row
   constexpr int KB = RB / 4, VB = RB / 16;
   constexpr int NK = D / 32;         // products over d
@@ -660,10 +685,10 @@ __global__ __launch_bounds__(256, kv_waves(D, BITS, R, FINE)) void k_kv_attend(K
 #pragma unroll
           for (int j = 0; j < DB; ++j) O[rt][j] *= f;
         });
+        if constexpr (FINE) weigh_fine(s, P[rt], fine[rt]);
+        else {
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          P[rt][e] = (_Float16)s[e];
-          if constexpr (FINE) fine[rt][e] = (_Float16)(s[e] - (float)P[rt][e]);
+          for (int e = 0; e < 8; ++e) P[rt][e] = (_Float16)s[e];
         }
       }
 
@@ -673,7 +698,7 @@ __global__ __launch_bounds__(256, kv_waves(D, BITS, R, FINE)) void k_kv_attend(K
       for (int e = 0; e < 8; ++e) v_unsigned<VB, BITS>(vr[e]);
 #pragma unroll
       for (int j = 0; j < DB; ++j) {
-        const h8 x = v_operand<VB, BITS>(vr, j);
+        const h8 x = j % 2 ? v_operand<VB, BITS, true>(vr, j) : v_operand<VB, BITS, false>(vr, j);
 #pragma unroll
         for (int rt = 0; rt < R; ++rt) {
           O[rt][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(x, P[rt], O[rt][j], 0, 0, 0);
