@@ -651,7 +651,8 @@ soniq_status soniq_kv_read(const soniq_kv_cache_t* cache, void* K_dev, int64_t k
  *   max_q      the largest n, at most 256; queries of a sequence from max_q
  *              on are not computed (their rows are left as they were)
  *   max_kv     the largest kv_len; only a hint for the split of the work,
- *              results hold for any lengths
+ *              results hold for any lengths (how a sequence's sum is split,
+ *              and so its rounding, depends on the call's other sequences)
  *   out_dev    device, type [T, q_heads, head_dim], strides as q's
  *   lse_dev    device, fp32 [T, q_heads]: log of the softmax's sum, or NULL
  *   work_dev   device, 16-byte aligned, at least the bytes that

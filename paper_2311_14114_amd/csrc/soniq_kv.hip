@@ -385,26 +385,71 @@ __device__ __forceinline__ uint32_t seen_bits(const KvAttend& a, int64_t t, int 
   return (uint32_t)v;
 }
 
-// How a launch is cut: parts of at least `chunk` positions each.
+// How a launch is cut.  Lengths count in pieces of 128 positions here.
 struct KvSplit {
-  int R;      // 16-row tiles a workgroup
-  int RB;     // workgroups over the rows
-  int parts;
-  int chunk;
+  int R;       // 16-row tiles a workgroup
+  int RB;      // workgroups over the rows
+  int parts;   // parts of a sequence, at most
+  int chunk;   // pieces of a part, at least
+  int cap;     // and at most, where `parts` allows (0: `chunk` as it is)
+  float per;   // parts of all sequences that make one workgroup a CU
+  int waves;   // workgroups a CU that are resident at once
+  bool pad;    // more LDS than is used, so that no more than two are
+  int least;   // and that the parts are to make, at least
 };
 
-// The positions of one part: [first, first + count).  A sequence longer than
-// the host was told takes longer parts.
+// Inclusive sums over the lanes of a wave.
+__device__ __forceinline__ uint32_t wave_scan(uint32_t x) {
+  x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xF, 0xF, false);  // row_shr 1, 2, 4, 8
+  x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xF, 0xF, false);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x114, 0xF, 0xF, false);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x118, 0xF, 0xF, false);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x142, 0xA, 0xF, false);  // row_bcast 15, 31
+  x += __builtin_amdgcn_update_dpp(0, x, 0x143, 0xC, 0xF, false);
+  return x;
+}
+__device__ __forceinline__ uint32_t wave_sum(uint32_t x) { return __builtin_amdgcn_readlane(wave_scan(x), 63); }
+
+__device__ __forceinline__ uint32_t pieces_of(int len) { return ((uint32_t)len + 127) / 128; }
+
+// Pieces a part takes, from the lengths themselves (lane b: those of sequence
+// b, 0 past the last; up to 64 sequences): the parts of all of them are to
+// make `least` workgroups a CU, or as many more up to all that are resident,
+// or twice, three times those, as `cap` asks for.  Floats only choose;
+// whatever they choose is cut exactly by part_of.
+__device__ __forceinline__ uint32_t kv_chunk(const KvSplit& sp, uint32_t pieces) {
+  if (sp.cap == 0) return sp.chunk;
+  const float total = (float)wave_sum(pieces), fl = (float)pieces, cap = (float)sp.cap, all = (float)sp.waves;
+  float w = fmaxf(ceilf(total / (sp.per * cap)), (float)sp.least);
+  if (w > all) w = ceilf(w / all) * all;
+  const float want = w * sp.per;
+  float c = fminf(fmaxf(ceilf(total / want), (float)sp.chunk), cap);
+  for (int i = 0; i < 8 && c < cap; ++i) {
+    const float n = (float)wave_sum((uint32_t)ceilf(fl * __builtin_amdgcn_rcpf(c) - 0.001f));
+    if (n <= want) break;
+    c = fminf(c + fmaxf(1.0f, floorf(c * 0.0625f)), cap);
+  }
+  return __builtin_amdgcn_readfirstlane((uint32_t)c);
+}
+// The same for one sequence: no more than `parts` of them.
+__device__ __forceinline__ uint32_t kv_chunk_of(uint32_t pieces, uint32_t chunk, int parts) {
+  return max(chunk, (pieces + parts - 1) / (uint32_t)parts);
+}
+
+// The positions of one part: [first, first + count).
 struct KvPart {
   int first, count, used;  // used: parts of this sequence that hold positions
 };
-__device__ __forceinline__ KvPart part_of(int len, int part, int parts, int chunk) {
-  // len < 2^31 and parts <= 2^22, so that nothing here passes 32 bits but the product
-  uint32_t c = ((uint32_t)len + parts - 1) / (uint32_t)parts;
-  c = max((c + 127) & ~127u, (uint32_t)chunk);
-  const uint64_t first = (uint64_t)part * c;
-  const int count = first >= (uint64_t)len ? 0 : (int)min((uint64_t)c, len - first);
-  return {(int)first, count, (int)(((uint32_t)len + c - 1) / c)};
+__device__ __forceinline__ KvPart part_of(int len, int part, int parts, uint32_t chunk) {
+  // len < 2^31, chunk <= 2^24, part < 2^22
+  const uint32_t pieces = pieces_of(len), c = kv_chunk_of(pieces, chunk, parts);
+  const uint64_t first = (uint64_t)part * c * 128;
+  const int count = first >= (uint64_t)len ? 0 : (int)min((uint64_t)c * 128, len - first);
+  return {(int)first, count, (int)((pieces + c - 1) / c)};
+}
+// Pieces of sequence `lane`, for the two calls above.
+__device__ __forceinline__ uint32_t kv_lane_pieces(const KvAttend& a, int lane) {
+  return lane < a.table.B ? pieces_of(kv_length(a.table, a.dims, a.kv_len[lane])) : 0;
 }
 
 // What a workgroup works on.
@@ -417,20 +462,32 @@ struct KvUnit {
 };
 // Workgroups of the same positions go to one XCD, one after the other.
 // False: there is nothing to do.
-__device__ __forceinline__ bool kv_unit(const KvAttend& a, const KvSplit& sp, KvUnit& u) {
+__device__ __forceinline__ bool kv_unit(const KvAttend& a, const KvSplit& sp, int lane, KvUnit& u) {
   const uint32_t id = blockIdx.x, x = id / 8;
   const int rb = (int)(x % sp.RB), unit = (int)(x / sp.RB) * 8 + (int)(id % 8);
   const int bp = unit / a.dims.heads;
   u.h = unit % a.dims.heads;
-  u.part = bp % sp.parts, u.b = bp / sp.parts;
-  if (u.b >= a.table.B) return false;
+  uint32_t chunk = sp.chunk;
+  if (sp.cap == 0) {
+    u.part = bp % sp.parts, u.b = bp / sp.parts;
+    if (u.b >= a.table.B) return false;
+  } else {
+    // the parts that hold positions, and one of each sequence without any, come first
+    const uint32_t pieces = kv_lane_pieces(a, lane);
+    chunk = kv_chunk(sp, pieces);
+    const uint32_t c = kv_chunk_of(pieces, chunk, sp.parts);
+    const uint32_t n = lane < a.table.B ? max((pieces + c - 1) / c, 1u) : 0, end = wave_scan(n);
+    u.b = __popcll(__ballot(end <= (uint32_t)bp));
+    if (u.b >= a.table.B) return false;
+    u.part = bp - (int)__builtin_amdgcn_readlane(end - n, u.b);
+  }
   u.span = kv_span(a.cu[u.b], a.cu[u.b + 1], a.T);
   u.nq = min(u.span.count, a.max_q);
   u.len = kv_length(a.table, a.dims, a.kv_len[u.b]);
   u.base = (int64_t)a.kv_len[u.b] - u.span.count;
   u.row0 = rb * 16 * sp.R;
   u.rows = min(u.nq * a.group - u.row0, 16 * sp.R);
-  u.pt = part_of(u.len, u.part, sp.parts, sp.chunk);
+  u.pt = part_of(u.len, u.part, sp.parts, chunk);
   return u.rows > 0 && (u.part == 0 || u.pt.count > 0);
 }
 
@@ -553,30 +610,36 @@ struct KvLds {
   KvRowInfo<16 * R> info;
 };
 
+template <int D>
+constexpr int kOutPitch = D + 4;  // of the outputs in LDS
+template <int D, int R>
+constexpr size_t kv_lds() {
+  constexpr size_t loop = sizeof(KvLds<D, R>), out = (size_t)4 * 16 * kOutPitch<D> * 4 + 4 * 16 * 8 + 64;
+  return loop > out ? loop : out;
+}
+
 // Waves a SIMD, by the registers that a row tile's outputs take.
-constexpr int kv_waves(int D, int BITS, int R) {
-  return D * R <= 64 || (D == 128 && R == 1 && BITS == 4) ? 4
-         : D * R <= 128 || (D == 128 && BITS == 4) ? 3 : 2;
+constexpr int kv_waves(int D, int R) {
+  return D * R <= 64 ? 5 : D * R <= 128 ? 4 : D * R <= 192 || D == 128 ? 3 : 2;
 }
 
 template <int D, int BITS, int R, bool FINE>
-__global__ __launch_bounds__(256, kv_waves(D, BITS, R)) void k_kv_attend(KvAttend a, KvSplit sp) {
+__global__ __launch_bounds__(256, kv_waves(D, R)) void k_kv_attend(KvAttend a, KvSplit sp) {
   constexpr int RB = D * BITS / 8;   // bytes of a cache row
   constexpr int KB = RB / 4, VB = RB / 16;
   constexpr int NK = D / 32;         // products over d
   constexpr int DB = D / 16;         // elements of d a lane holds, and V operands
-  constexpr int OP = D + 4;          // pitch of the outputs in LDS
-  constexpr size_t kLdsLoop = sizeof(KvLds<D, R>), kLdsOut = (size_t)4 * 16 * OP * 4 + 4 * 16 * 8 + 64;
-  __shared__ __align__(16) uint8_t lds_bytes[kLdsLoop > kLdsOut ? kLdsLoop : kLdsOut];
+  constexpr int OP = kOutPitch<D>;
+  __shared__ __align__(16) uint8_t lds_bytes[kv_lds<D, R>()];
   KvLds<D, R>& L = *reinterpret_cast<KvLds<D, R>*>(lds_bytes);
 
   KvUnit un;
-  if (!kv_unit(a, sp, un)) return;
+  if (!kv_unit(a, sp, threadIdx.x % 64, un)) return;
   const int h = un.h, G = a.group, nq = un.nq, row0 = un.row0;
   const KvSpan span = un.span;
   const KvPart pt = un.pt;
   const int64_t base = un.base;
-  const int tid = threadIdx.x, lane = tid % 64, c = lane % 16, kb = lane / 16;
+  int tid = threadIdx.x, lane = tid % 64, c = lane % 16, kb = lane / 16;
   const int wave = __builtin_amdgcn_readfirstlane(tid / 64);  // uniform, and known to be
 
   f4 O[R][DB];
@@ -611,18 +674,20 @@ __global__ __launch_bounds__(256, kv_waves(D, BITS, R)) void k_kv_attend(KvAtten
   // and V on their way.
   auto prepare = [&](int s0, auto first) {
     const int n = min(pt.count - s0, kSub);
+    int x = tid;
+    asm volatile("" : "+v"(x));  // nothing of this is kept over the loop
     KvFind f;
     KvQuery<D, BITS, R> q;
-    f.find(a, un, pt.first + s0, n, tid);
-    if constexpr (decltype(first)::value) q.load(a, un, tid);
-    f.rows(a, un, n, tid, L.p);
+    f.find(a, un, pt.first + s0, n, x);
+    if constexpr (decltype(first)::value) q.load(a, un, x);
+    f.rows(a, un, n, x, L.p);
     lds_barrier();
     if (wave < (n + 31) / 32) {
       load_k(wave);
       load_v(wave);
     }
-    if constexpr (decltype(first)::value) q.stage(a, un, tid, L.q, L.info);
-    f.scales(n, tid, L.p);
+    if constexpr (decltype(first)::value) q.stage(a, un, x, L.q, L.info);
+    f.scales(n, x, L.p);
     lds_barrier();
   };
 
@@ -714,6 +779,7 @@ __global__ __launch_bounds__(256, kv_waves(D, BITS, R)) void k_kv_attend(KvAtten
   }
 
   // ---- the four waves meet, one row tile at a time
+  asm volatile("" : "+v"(tid), "+v"(c), "+v"(kb));  // nor of this
   float* out = reinterpret_cast<float*>(lds_bytes);       // [wave][16][OP]
   float* ml = out + 4 * 16 * OP;                          // [wave][16][2]
   const bool direct = pt.used <= 1;
@@ -783,7 +849,8 @@ __global__ __launch_bounds__(256) void k_kv_join(KvAttend a, KvSplit sp) {
   if (b >= a.table.B) return;
   const KvSpan span = kv_span(a.cu[b], a.cu[b + 1], a.T);
   if (t < span.first || t - span.first >= min(span.count, a.max_q)) return;
-  const KvPart pt = part_of(kv_length(a.table, a.dims, a.kv_len[b]), 0, sp.parts, sp.chunk);
+  const uint32_t chunk = sp.cap == 0 ? sp.chunk : kv_chunk(sp, kv_lane_pieces(a, lane));
+  const KvPart pt = part_of(kv_length(a.table, a.dims, a.kv_len[b]), 0, sp.parts, chunk);
   if (pt.used <= 1) return;  // written where it was computed
   const float* w = a.work + x * sp.parts * D;
   const float* wml = a.work + (int64_t)a.T * a.q_heads * sp.parts * D + x * sp.parts * 2;
@@ -841,28 +908,41 @@ __global__ __launch_bounds__(256) void k_kv_join(KvAttend a, KvSplit sp) {
   if (lane == 0 && a.lse) a.lse[x] = l == 0.0f ? -INFINITY : (m + __log2f(l)) * 0.693147181f;
 }
 
-// Rows a workgroup takes, and how the positions are cut.  At least about a
-// thousand workgroups where the positions give them (two to four a CU are
-// resident), at most about eight thousand, and parts of at most 1024
-// positions a row tile otherwise, so that ragged lengths level out.  A part
-// costs its workgroup a start of several dependent loads, and 4 bytes an
-// output written and read again (eight sequences of 3001 to 8191 positions,
-// 8 heads, 96 rows: 62 us with a target of 1024 workgroups, 66 with 2048, 78
-// with 4096; 512 rows: 192, 188, 187).  Four row tiles a wave spill.
+// Rows a workgroup takes, and how the positions are cut.  A part costs its
+// workgroup a start of several dependent loads, and 4 bytes an output written
+// and read again; and parts that are not all resident end unevenly.  So up to
+// 64 sequences are cut on the device, by their lengths (see kv_chunk).  Parts
+// have at most 1024 positions a row tile, and about eight thousand workgroups
+// a call where that gives longer ones.  Two row tiles and short parts: two
+// workgroups a CU, held there by LDS that nobody uses, finish sooner than
+// three with shorter parts yet.  Eight sequences of 3001 to 8191 positions, 8
+// heads of 128, 8 bits, us a call in a graph:
+//   rows  four workgroups a CU by the longest  by lengths, two   three
+//     20                 35.0                      28.2          28.8
+//     64                 49.2                      42            39.6
+//     96                 65.5                      66            53.5
+// (96 rows, 4 bits, fp16: 61.2, 67.7, 55.6.)
+// More sequences, or few positions: by the longest one's length, about a
+// thousand workgroups.  Four row tiles a wave spill.
 KvSplit kv_split(const KvDims& d, int32_t q_heads, int64_t B, int64_t max_q, int64_t max_kv) {
   const int64_t rows = max_q * (q_heads / d.heads);
   KvSplit s;
   s.R = rows <= 16 ? 1 : 2;
   s.RB = (int)((rows + 16 * s.R - 1) / (16 * s.R));
-  const int64_t units = B * d.heads * s.RB;
-  auto up = [](int64_t x) { return (x + 127) / 128 * 128; };
-  max_kv = max_kv < 1 ? 1 : max_kv;
-  const int64_t cap = std::max<int64_t>(1024 * s.R, up(max_kv * units / 8192));
-  int64_t chunk = std::min(std::max<int64_t>(up(max_kv * units / 1024), 128), cap);
-  int64_t parts = (max_kv + chunk - 1) / chunk;
-  parts = std::max<int64_t>(1, std::min(parts, ((int64_t)1 << 22) / units));
+  const int64_t units = B * d.heads * s.RB, pieces = max_kv < 1 ? 1 : (max_kv + 127) / 128;
+  auto over = [&](int64_t n) { return (pieces * units + n - 1) / n; };
+  const bool by_lengths = B <= 64 && pieces * units > 512;
+  const int64_t cap = std::max<int64_t>(8 * s.R, over(8192));
+  const int64_t chunk = std::min(over(1024), cap);
+  const int64_t parts = std::min((pieces + chunk - 1) / chunk, std::max<int64_t>(((int64_t)1 << 22) / units, 1));
   s.chunk = (int)chunk;
   s.parts = (int)parts;
+  s.cap = by_lengths && parts > 1 ? (int)cap : 0;
+  s.per = 256.0f / ((float)d.heads * (float)s.RB);
+  s.waves = kv_waves(d.head_dim, s.R);
+  s.pad = s.R == 2 && s.waves > 2 && by_lengths && over(3 * 256) <= 9;
+  if (s.pad) s.waves = 2;
+  s.least = s.R == 2 ? s.waves : 2;
   return s;
 }
 
@@ -870,16 +950,20 @@ template <int D, int BITS>
 void launch_attend(const KvAttend& a, const KvSplit& s, hipStream_t stream) {
   const int64_t u = (int64_t)a.table.B * a.dims.heads * s.parts;
   const dim3 grid((unsigned)((u + 7) / 8 * 8 * s.RB)), block(256);
+  constexpr size_t kTwo = 56 << 10;  // of 160 KB
+  const size_t pad = s.pad ? kTwo - std::min(kTwo, kv_lds<D, 2>()) : 0;
   if (a.type == SONIQ_F16) {
     if (s.R == 1) k_kv_attend<D, BITS, 1, true><<<grid, block, 0, stream>>>(a, s);
-    else k_kv_attend<D, BITS, 2, true><<<grid, block, 0, stream>>>(a, s);
+    else k_kv_attend<D, BITS, 2, true><<<grid, block, pad, stream>>>(a, s);
   } else {
     if (s.R == 1) k_kv_attend<D, BITS, 1, false><<<grid, block, 0, stream>>>(a, s);
-    else k_kv_attend<D, BITS, 2, false><<<grid, block, 0, stream>>>(a, s);
+    else k_kv_attend<D, BITS, 2, false><<<grid, block, pad, stream>>>(a, s);
   }
   if (s.parts <= 1) return;
   const int64_t x = (int64_t)a.T * a.q_heads;
-  if (s.parts <= 8) k_kv_join<D, 1><<<(unsigned)((x + 3) / 4), 256, 0, stream>>>(a, s);
+  // a wave a row, or four where rows are few and parts many (16 sequences of
+  // 501 to 2191 positions, 4096 rows: 24.7 us a call and 29.1)
+  if (s.parts <= 8 || (s.parts <= 32 && x >= 2048)) k_kv_join<D, 1><<<(unsigned)((x + 3) / 4), 256, 0, stream>>>(a, s);
   else k_kv_join<D, 4><<<(unsigned)x, 256, 0, stream>>>(a, s);
 }
 

@@ -251,6 +251,22 @@ def test_many_sequences(max_kv):
     _check_attention(cache, h, q, table, cu, lens, 8, max_q=9, max_kv=max_kv)
 
 
+@pytest.mark.parametrize("B", [3, 40, 64, 65])
+@pytest.mark.parametrize("longest,rows", [(9000, 1), (1500, 40)])
+@pytest.mark.parametrize("max_kv", [None, 128, 1 << 20])
+def test_parts_of_very_different_lengths(B, longest, rows, max_kv):
+    """One long sequence among short and empty ones, which the lengths
+    themselves cut, with hints far off on both sides."""
+    r = np.random.default_rng(24)
+    new = [rows] + r.integers(0, rows + 1, B - 1).tolist()
+    lens = [longest] + [int(n * (k % 3 > 0) + r.choice([0, 0, 1, 127, 129, 700])) for k, n in enumerate(new[1:])]
+    pages, table = _tables(r, lens, 128)
+    cache, h = _random_cache(r, pages, 128, 2, 64, 4)
+    cu = np.concatenate(([0], np.cumsum(new))).tolist()
+    q = torch.from_numpy(r.standard_normal((sum(new) + 1, 2, 64)).astype(np.float32)).to(torch.float16).cuda()
+    _check_attention(cache, h, q, table, cu, lens, 4, max_q=rows, max_kv=max_kv)
+
+
 def test_two_graphs_share_a_workspace():
     """Two layers' attention captured on one workspace, replayed in turn, with
     eager work on it between the replays."""
