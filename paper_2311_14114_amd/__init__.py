@@ -540,59 +540,64 @@ def _raw_stream(stream, device: int):
     return torch._C._cuda_getCurrentRawStream(device)
 
 
-def _empty(shape, dtype, device, stream):
-    """Memory that a call on `stream` writes: taken on that stream, so that it
-    is neither in use elsewhere before nor given away too early after."""
+def _empty(like, shape, dtype, stream):
+    """Memory on like's device that a call on `stream` writes: taken on that
+    stream, so that it is neither in use elsewhere before nor given away too
+    early after."""
     if stream is None:
-        return torch.empty(shape, dtype=dtype, device=device)
-    s = torch.cuda.ExternalStream(int(stream), device) if int(stream) else torch.cuda.default_stream(device)
+        return like.new_empty(shape, dtype=dtype)
+    s = torch.cuda.ExternalStream(int(stream), like.device) if int(stream) else torch.cuda.default_stream(like.device)
     with torch.cuda.stream(s):
-        return torch.empty(shape, dtype=dtype, device=device)
+        return like.new_empty(shape, dtype=dtype)
 
 
-def _refuse(t, what: str, d: int, dtype, dim: int):
+def _is(t, what: str, d: int, dtype, dim: int):
+    """Refuses what is not a tensor of that type and number of dimensions on
+    device d.  The checks below come here once something is amiss."""
     if not isinstance(t, torch.Tensor) or not t.is_cuda:
         raise TypeError(f"{what} must be a device tensor")
     if t.get_device() != d:
         raise ValueError(f"{what} is on {t.device}, the current device is cuda:{d}")
     if t.dtype is not dtype:
         raise TypeError(f"{what} must be {dtype}")
-    raise TypeError(f"{what} must have {dim} dimensions")
-
-
-def _is(t, what: str, d: int, dtype, dim: int):
-    """A tensor of that type and number of dimensions on device d."""
-    try:
-        if t.get_device() == d and t.dtype is dtype and t.dim() == dim:
-            return
-    except AttributeError:
-        pass
-    _refuse(t, what, d, dtype, dim)
+    if t.dim() != dim:
+        raise TypeError(f"{what} must have {dim} dimensions")
 
 
 def _vector(t, what: str, d: int, dtype, n: int) -> int:
     """Address of a contiguous tensor of n elements."""
+    try:
+        if t.dtype is dtype and t.get_device() == d and t.shape == (n,) and t.is_contiguous():
+            return t.data_ptr()
+    except AttributeError:
+        pass
     _is(t, what, d, dtype, 1)
-    if t.shape[0] != n or not t.is_contiguous():
-        raise ValueError(f"{what} must be a contiguous tensor of {n} elements")
-    return t.data_ptr()
+    raise ValueError(f"{what} must be a contiguous tensor of {n} elements")
 
 
-def _ld(t, what: str, M: int, K: int) -> int:
-    """Leading dimension of an [M, K] tensor with unit column stride (a stride
-    says nothing where there is one row, or one column)."""
+def _rows(t, what: str, d: int, dtype):
+    """(M, K, leading dimension, address) of an [M, K] tensor with unit column
+    stride (a stride says nothing where there is one row, or one column)."""
+    try:
+        if t.dtype is dtype and t.get_device() == d:
+            M, K = t.shape
+            ld, unit = t.stride()
+            if unit == 1 and ld >= K:
+                return M, K, ld, t.data_ptr()
+    except (AttributeError, ValueError):
+        pass
+    _is(t, what, d, dtype, 2)
+    M, K = t.shape
     ld, unit = t.stride()
     if unit != 1 and K > 1:
         raise TypeError(f"{what} must have unit column stride")
-    if M <= 1:
-        return ld if ld > K else K
-    if ld < K:
+    if ld < K and M > 1:
         raise TypeError(f"{what} has rows that overlap")
-    return ld
+    return M, K, max(ld, K), t.data_ptr()
 
 
 def _type_of(t, what: str) -> int:
-    code = _TYPES.get(t.dtype)
+    code = _TYPES.get(getattr(t, "dtype", t))
     if code is None:
         raise TypeError(f"{what} must be float32, bfloat16 or float16")
     return code
@@ -604,36 +609,43 @@ def soniq_quantize_rows(A, out=None, scales=None, stream=None):
     weight matrix.  Returns (codes int8 [M, K], scales float32 [M])."""
     d = _device(A, "A")
     ta = _type_of(A, "A")
-    _is(A, "A", d, A.dtype, 2)
-    M, K = A.shape
-    lda = _ld(A, "A", M, K)
+    M, K, lda, a = _rows(A, "A", d, A.dtype)
     if out is None:
-        out = _empty((M, -(-K // 16) * 16), torch.int8, A.device, stream)[:, :K]
+        ldq = -(-K // 16) * 16
+        out = _empty(A, (M, ldq), torch.int8, stream)[:, :K]
+        q = out.data_ptr()
     else:
-        _is(out, "out", d, torch.int8, 2)
-        if out.shape != A.shape:
+        Mq, Kq, ldq, q = _rows(out, "out", d, torch.int8)
+        if Mq != M or Kq != K:
             raise ValueError("out must have A's shape")
     if scales is None:
-        scales = _empty(M, torch.float32, A.device, stream)
+        scales = _empty(A, (M,), torch.float32, stream)
     s = _vector(scales, "scales", d, torch.float32, M)
-    _check(_lib.soniq_quantize_rows(A.data_ptr(), ta, M, K, lda, out.data_ptr(), _ld(out, "out", M, K), s,
-                                     _raw_stream(stream, d)))
+    _check(_lib.soniq_quantize_rows(a, ta, M, K, lda, q, ldq, s, _raw_stream(stream, d)))
     return out, scales
 
 
-def _i8_operands(W, s_w, bias, d, M, K, out, dtype, device, stream):
-    _is(W, "W", d, torch.int8, 2)
-    N, Kw = W.shape
+def _i8_weights(W, s_w, bias, d, K):
+    """N, then the C arguments W, ldw, s_w, bias."""
+    N, Kw, ldw, w = _rows(W, "W", d, torch.int8)
     if Kw != K:
         raise ValueError("W has the wrong number of input channels")
+    return N, w, ldw, _vector(s_w, "s_w", d, torch.float32, N), \
+        None if bias is None else _vector(bias, "bias", d, torch.float32, N)
+
+
+def _i8_out(A, M, N, out, dtype, d, stream):
+    """out, then the C arguments Y, y_type, ldy."""
     if out is None:
-        out = _empty((M, N), torch.bfloat16 if dtype is None else dtype, device, stream)
-    else:
-        _is(out, "out", d, out.dtype if dtype is None else dtype, 2)
-        if out.shape[0] != M or out.shape[1] != N:
-            raise ValueError("out must be [M, N]")
-    return (N, W.data_ptr(), _ld(W, "W", N, K), _vector(s_w, "s_w", d, torch.float32, N),
-            None if bias is None else _vector(bias, "bias", d, torch.float32, N), out)
+        dtype = torch.bfloat16 if dtype is None else dtype
+        code = _type_of(dtype, "dtype")
+        out = _empty(A, (M, N), dtype, stream)
+        return out, out.data_ptr(), code, N
+    code = _type_of(out, "out")
+    My, Ny, ldy, y = _rows(out, "out", d, out.dtype if dtype is None else dtype)
+    if My != M or Ny != N:
+        raise ValueError("out must be [M, N]")
+    return out, y, code, ldy
 
 
 def soniq_i8_gemm(A, s_a, W, s_w, bias=None, out=None, dtype=None, stream=None):
@@ -641,12 +653,11 @@ def soniq_i8_gemm(A, s_a, W, s_w, bias=None, out=None, dtype=None, stream=None):
     W [N, K] with float32 scales per row; Y [M, N] of `dtype` (bfloat16 unless
     given).  Returns Y."""
     d = _device(A, "A")
-    _is(A, "A", d, torch.int8, 2)
-    M, K = A.shape
+    M, K, lda, a = _rows(A, "A", d, torch.int8)
     sa = _vector(s_a, "s_a", d, torch.float32, M)
-    N, w, ldw, sw, b, out = _i8_operands(W, s_w, bias, d, M, K, out, dtype, A.device, stream)
-    _check(_lib.soniq_i8_gemm(A.data_ptr(), _ld(A, "A", M, K), sa, w, ldw, sw, b, M, N, K, out.data_ptr(),
-                               _type_of(out, "out"), _ld(out, "out", M, N), _raw_stream(stream, d)))
+    N, w, ldw, sw, b = _i8_weights(W, s_w, bias, d, K)
+    out, y, ty, ldy = _i8_out(A, M, N, out, dtype, d, stream)
+    _check(_lib.soniq_i8_gemm(a, lda, sa, w, ldw, sw, b, M, N, K, y, ty, ldy, _raw_stream(stream, d)))
     return out
 
 
@@ -657,16 +668,18 @@ def soniq_quantize_i8_gemm_workspace(M: int, K: int) -> int:
     return n.value
 
 
-def _work(work, need: int, d: int, device, stream):
+def _work(work, need: int, d: int, like, stream):
+    """The workspace, its address and size: the caller's, or one of `need`
+    bytes that lives until the call returns."""
     if work is None:
         if need == 0:
-            return None, 0, None
-        work = _empty(need, torch.uint8, device, stream)
-        return work.data_ptr(), need, work
+            return None, None, 0
+        work = _empty(like, (need,), torch.uint8, stream)
+        return work, work.data_ptr(), need
     _is(work, "work", d, torch.uint8, 1)
     if not work.is_contiguous():
         raise ValueError("work must be contiguous")
-    return work.data_ptr(), work.numel(), work
+    return work, work.data_ptr(), work.numel()
 
 
 def soniq_quantize_i8_gemm(A, W, s_w, bias=None, out=None, dtype=None, work=None, stream=None):
@@ -675,13 +688,11 @@ def soniq_quantize_i8_gemm(A, W, s_w, bias=None, out=None, dtype=None, work=None
     bytes (allocated when None).  Returns Y."""
     d = _device(A, "A")
     ta = _type_of(A, "A")
-    _is(A, "A", d, A.dtype, 2)
-    M, K = A.shape
-    lda = _ld(A, "A", M, K)
-    N, w, ldw, sw, b, out = _i8_operands(W, s_w, bias, d, M, K, out, dtype, A.device, stream)
-    wp, wn, work = _work(work, soniq_quantize_i8_gemm_workspace(M, K), d, A.device, stream)
-    _check(_lib.soniq_quantize_i8_gemm(A.data_ptr(), ta, lda, w, ldw, sw, b, M, N, K, out.data_ptr(),
-                                        _type_of(out, "out"), _ld(out, "out", M, N), wp, wn,
+    M, K, lda, a = _rows(A, "A", d, A.dtype)
+    N, w, ldw, sw, b = _i8_weights(W, s_w, bias, d, K)
+    out, y, ty, ldy = _i8_out(A, M, N, out, dtype, d, stream)
+    work, wp, wn = _work(work, soniq_quantize_i8_gemm_workspace(M, K), d, A, stream)
+    _check(_lib.soniq_quantize_i8_gemm(a, ta, lda, w, ldw, sw, b, M, N, K, y, ty, ldy, wp, wn,
                                         _raw_stream(stream, d)))
     return out
 
@@ -736,24 +747,26 @@ def _kv_batch(cache, page_table, cu, lengths, what):
     d = cache.device_index
     if torch._C._cuda_getDevice() != d:
         raise ValueError(f"the cache is on {cache.device}, the current device is another one")
-    i32 = torch.int32
-    _is(page_table, "page_table", d, i32, 2)
-    B, width = page_table.shape
-    return (d, B, width, _ld(page_table, "page_table", B, width), page_table.data_ptr(),
-            _vector(cu, "cu", d, i32, B + 1), _vector(lengths, what, d, i32, B))
+    B, width, ld, table = _rows(page_table, "page_table", d, torch.int32)
+    return (d, B, width, ld, table, _vector(cu, "cu", d, torch.int32, B + 1),
+            _vector(lengths, what, d, torch.int32, B))
 
 
 def _kv_rows(t, what: str, d: int, heads: int, head_dim: int):
-    """Type code and strides of a [T, heads, head_dim] tensor."""
+    """Tokens, type code, strides and address of a [T, heads, head_dim] tensor."""
     code = _type_of(t, what)
-    _is(t, what, d, t.dtype, 3)
-    _, h, n = t.shape
+    try:
+        T, h, n = t.shape
+    except (AttributeError, ValueError):
+        T = h = n = -1
+    if t.get_device() != d or T < 0:
+        _is(t, what, d, t.dtype, 3)
     if h != heads or n != head_dim:
         raise ValueError(f"{what} must be [T, {heads}, {head_dim}]")
     ts, hs, unit = t.stride()
     if unit != 1:
         raise TypeError(f"{what} must have unit stride in its last dimension")
-    return code, ts, hs
+    return T, code, ts, hs, t.data_ptr()
 
 
 def _kv_out(t, what: str, ts: int, hs: int):
@@ -770,13 +783,12 @@ def soniq_kv_write(cache: KVCache, K, V, page_table, cu, start, stream=None) -> 
     page_table[b] names.  page_table int32 [B, width], cu int32 [B + 1],
     start int32 [B], all on the device."""
     d, B, width, ld, table, cu, start = _kv_batch(cache, page_table, cu, start, "start")
-    tk, kts, khs = _kv_rows(K, "K", d, cache.heads, cache.head_dim)
-    tv, vts, vhs = _kv_rows(V, "V", d, cache.heads, cache.head_dim)
-    T = K.shape[0]
-    if tk != tv or T != V.shape[0]:
+    T, tk, kts, khs, k = _kv_rows(K, "K", d, cache.heads, cache.head_dim)
+    Tv, tv, vts, vhs, v = _kv_rows(V, "V", d, cache.heads, cache.head_dim)
+    if tk != tv or T != Tv:
         raise ValueError("K and V must have one type and one number of tokens")
-    _check(_lib.soniq_kv_write(cache._ref, K.data_ptr(), kts, khs, V.data_ptr(), vts, vhs, tk, T, table, ld, width,
-                                B, cu, start, _raw_stream(stream, d)))
+    _check(_lib.soniq_kv_write(cache._ref, k, kts, khs, v, vts, vhs, tk, T, table, ld, width, B, cu, start,
+                                _raw_stream(stream, d)))
 
 
 def soniq_kv_read(cache: KVCache, page_table, cu, start, tokens: int, dtype=None, out=None, stream=None):
@@ -788,19 +800,21 @@ def soniq_kv_read(cache: KVCache, page_table, cu, start, tokens: int, dtype=None
     heads, D = cache.heads, cache.head_dim
     if out is None:
         dtype = torch.bfloat16 if dtype is None else dtype
-        K, V = _empty((2, tokens, heads, D), dtype, cache.device, stream).unbind(0)
-        tk, kts, khs = _type_of(K, "dtype:"), heads * D, D
-        vts, vhs = kts, khs
+        tk = _type_of(dtype, "dtype")
+        K, V = _empty(cache.k, (2, tokens, heads, D), dtype, stream).unbind(0)
+        kts = vts = heads * D
+        khs = vhs = D
+        k, v = K.data_ptr(), V.data_ptr()
     else:
         K, V = out
-        tk, kts, khs = _kv_rows(K, "K", d, heads, D)
-        tv, vts, vhs = _kv_rows(V, "V", d, heads, D)
-        if tk != tv or K.shape[0] != tokens or V.shape[0] != tokens or (dtype is not None and K.dtype is not dtype):
+        Tk, tk, kts, khs, k = _kv_rows(K, "K", d, heads, D)
+        Tv, tv, vts, vhs, v = _kv_rows(V, "V", d, heads, D)
+        if tk != tv or Tk != tokens or Tv != tokens or (dtype is not None and K.dtype is not dtype):
             raise ValueError("K and V must have one type (dtype) and `tokens` rows")
         _kv_out(K, "K", kts, khs)
         _kv_out(V, "V", vts, vhs)
-    _check(_lib.soniq_kv_read(cache._ref, K.data_ptr(), kts, khs, V.data_ptr(), vts, vhs, tk, tokens, table, ld,
-                               width, B, cu, start, _raw_stream(stream, d)))
+    _check(_lib.soniq_kv_read(cache._ref, k, kts, khs, v, vts, vhs, tk, tokens, table, ld, width, B, cu, start,
+                               _raw_stream(stream, d)))
     return K, V
 
 
@@ -833,18 +847,15 @@ def soniq_kv_attention(cache: KVCache, q, page_table, cu, kv_len, scale=None, ma
     work: a uint8 device tensor of soniq_kv_attention_workspace(...) bytes
     (allocated when None).  Returns out (like q)."""
     d, B, width, ld, table, cu, kv_len = _kv_batch(cache, page_table, cu, kv_len, "kv_len")
-    code = _type_of(q, "q")
-    _is(q, "q", d, q.dtype, 3)
-    T, heads, D = q.shape
-    qts, qhs, unit = q.stride()
-    if D != cache.head_dim or unit != 1:
-        raise ValueError(f"q must be [T, q_heads, {cache.head_dim}] with unit stride in its last dimension")
+    D = cache.head_dim
+    heads = q.shape[1] if isinstance(q, torch.Tensor) and q.dim() == 3 else 0
+    T, code, qts, qhs, qp = _kv_rows(q, "q", d, heads, D)
     if out is None:
-        out = _empty((T, heads, D), q.dtype, cache.device, stream)
+        out = _empty(q, (T, heads, D), q.dtype, stream)
         ots, ohs = heads * D, D
     else:
-        to, ots, ohs = _kv_rows(out, "out", d, heads, D)
-        if to != code or out.shape[0] != T:
+        To, to, ots, ohs, _ = _kv_rows(out, "out", d, heads, D)
+        if to != code or To != T:
             raise ValueError("out must have q's shape and type")
         _kv_out(out, "out", ots, ohs)
     words, bits = 0, None
@@ -861,9 +872,9 @@ def soniq_kv_attention(cache: KVCache, q, page_table, cu, kv_len, scale=None, ma
         max_q = max(T, 1)
     if max_kv is None:
         max_kv = width * cache.page_size
-    wp, wn, work = _work(work, soniq_kv_attention_workspace(cache, T, heads, B, max_q, max_kv), d, cache.device, stream)
-    _check(_lib.soniq_kv_attention(cache._ref, q.data_ptr(), qts, qhs, code, T, heads, table, ld, width, B, cu,
-                                    kv_len, bits, words, D ** -0.5 if scale is None else scale, max_q, max_kv,
-                                    out.data_ptr(), ots, ohs, None if lse is None else lse.data_ptr(), wp, wn,
-                                    _raw_stream(stream, d)))
+    need = _kv_work(cache.pages, cache.page_size, cache.heads, D, cache.bits, T, heads, B, max_q, max_kv)
+    work, wp, wn = _work(work, need, d, q, stream)
+    _check(_lib.soniq_kv_attention(cache._ref, qp, qts, qhs, code, T, heads, table, ld, width, B, cu, kv_len, bits,
+                                    words, D ** -0.5 if scale is None else scale, max_q, max_kv, out.data_ptr(), ots,
+                                    ohs, None if lse is None else lse.data_ptr(), wp, wn, _raw_stream(stream, d)))
     return out

@@ -457,7 +457,7 @@ def test_binding_refusals():
     bad = [(TypeError, lambda: att(t=t.long())), (ValueError, lambda: att(cu=cu[:1])), (TypeError, lambda: att(ln=ln.cpu())),
            (sq.SoniqError, lambda: att(q=q.float())), (TypeError, lambda: att(q=q.double())),
            (sq.SoniqError, lambda: att(q=q[:, :3])), (ValueError, lambda: att(q=q[..., :32])),
-           (ValueError, lambda: att(q=q.transpose(1, 2).contiguous().transpose(1, 2))),
+           (TypeError, lambda: att(q=q.transpose(1, 2).contiguous().transpose(1, 2))),
            (TypeError, lambda: att(mask=torch.zeros((3, 1), dtype=torch.int32, device="cuda"))),
            (ValueError, lambda: att(mask=torch.zeros((2, 1), dtype=torch.int64, device="cuda"))),
            (sq.SoniqError, lambda: att(mask=torch.zeros((3, 5), dtype=torch.int64, device="cuda"))),
