@@ -1,11 +1,19 @@
 // gfx950 kernels of the 8-bit linear layers with one scale per token and per
-// output channel.
+// output channel:
+//   Y[m,n] = (float(sum_k Qa[m,k] Qw[n,k]) * s_a[m]) * s_w[n] + bias[n],
+//   s_a[m] = max_k |A[m,k]| / 127,  Qa = rint(A / s_a).
 //
 //   k_rows       codes and scales of rows, one wave or one workgroup a row
-//   k_i8_skinny  few tokens: bound by the weights' bytes; both operands from
-//                memory to registers, the waves of a workgroup split K
-//   k_i8_tile    many tokens: bound by the matrix cores; operands staged
-//                through LDS
+//   k_i8_fused   one to four tokens, quantized where they are used: one launch
+//   k_i8_skinny  up to 64 tokens: bound by the weights' bytes; the waves of a
+//                workgroup split K, each with its own part of LDS
+//   k_i8_tile    more tokens: bound by LDS where tiles are few and small, by
+//                the matrix cores else; operands staged through LDS
+//   k_i8_short   more tokens of fewer than 16 channels
+//
+// The integer sums are exact, so no split or order of K changes a bit.
+// Measured figures in this file are of one MI355X; times "in a graph" leave
+// out the host's part of a call.
 #include "soniq_serve.h"
 #include "soniq_values.h"
 
@@ -75,7 +83,11 @@ __device__ __forceinline__ uint32_t wave_max(uint32_t m) {
 
 // T threads a row, 256 a workgroup.  A row of up to 8 * T * kHeld elements
 // stays in registers between its maximum and its codes; longer ones are read
-// again for the rest.
+// again for the rest.  Bytes bound it where rows are many: 4096 x 11008 bf16
+// take 34 us, 136 MB at 4.0 TB/s (a large copy reaches 4.8; the part of a row
+// past the 8192 held elements comes from L2); 8192 x 8192 51 us, 202 MB at
+// 4.0.  Few rows take two dependent trips to memory and a barrier: 40 x 4096
+// 4.3 us.
 template <int TYPE, int T>
 __global__ __launch_bounds__(256) void k_rows(const typename Value<TYPE>::T* A, int64_t M, int K, int64_t lda,
                                               int8_t* Q, int64_t ldq, float* s) {
@@ -134,6 +146,7 @@ __device__ __forceinline__ float scaled(int acc, float sa, float sw) {
 // lanes in different rows (loading operands as they are took 60 accesses an
 // instruction and half the speed).  So each wave turns its segments through
 // its own part of LDS, with no barrier; sums meet in LDS at the end.
+// 40 x 11008 x 4096 take 11.4 us: 45 MB of weights at 4.0 TB/s.
 template <int A8, int NT>
 __global__ __launch_bounds__(512) void k_i8_skinny(I8Gemm g) {
   constexpr int MT = (A8 + 1) / 2, NL = A8 + 2 * NT;           // loads a lane and segment
@@ -234,7 +247,8 @@ __global__ __launch_bounds__(512) void k_i8_skinny(I8Gemm g) {
 // One to four tokens with their quantization in the same launch: every
 // workgroup makes the codes for itself (at most kFusedMost elements, 32 a
 // thread), in LDS, while its first weights are on their way.  16 output
-// channels a workgroup, K over the waves as above.
+// channels a workgroup, K over the waves as above.  1 x 4096 x 4096 takes
+// 6.1 us: 17 MB at 2.8 TB/s, half of it the way from the launch to the codes.
 constexpr int kFusedMost = 16384;
 
 template <int TYPE>
@@ -449,6 +463,14 @@ __device__ __forceinline__ void tile_out(const I8Gemm& g, const v16i (&acc)[TM][
 // with its own buffers, and the first adds the second's sums before it stores.
 // Few tiles leave a CU with one workgroup, whose one stage in flight does not
 // cover the memory's latency.
+//
+// 8192^3 takes 455 to 470 us, 2340 to 2410 TOPS (the matrix cores busy 0.64
+// of the time; a library's product of int8 matrices reached 2066 to 2430 on
+// this card), 4096 x 4096 x 11008 154 us, 2400.  Small tiles are bound by
+// LDS: a stage of 64x128 writes 24 KB and reads 48, some 770 of the 900
+// cycles that it takes (301 x 4099 x 4091: 13.6 us); two stages in flight a
+// set, or four sets, changed nothing.  Weights' rows that do not start at
+// multiples of 16 bytes take two lines a load: 19 us there.
 template <int BM, int BN, bool CLAMP, int SETS>
 __global__ __launch_bounds__(256 * SETS, BM * BN * SETS > 128 * 128 ? 1 : 2) void k_i8_tile(I8Gemm g, int tm, int tn) {
   constexpr int TM = BM / 64, TN = BN / 64;        // 32x32 tiles a wave
@@ -456,15 +478,17 @@ __global__ __launch_bounds__(256 * SETS, BM * BN * SETS > 128 * 128 ? 1 : 2) voi
   __shared__ __align__(16) int8_t lds_all[SETS][2][(BM + BN) * 128];
 
   // Workgroup b runs on XCD b % 8: each XCD takes a contiguous run of the
-  // tile order, columns of four row blocks, so that its L2 serves the rows
-  // that its tiles share.
+  // tile order, columns of up to four row blocks (bands of one height: 600 x
+  // 4096 x 4096 takes 18.3 us, 19.2 with two fours and a two), so that its L2
+  // serves the rows that its tiles share.
   int bm, bn;
   {
     const int total = tm * tn, per = (total + 7) / 8;
     const int t = (int)(blockIdx.x % 8) * per + (int)(blockIdx.x / 8);
     if ((int)(blockIdx.x / 8) >= per || t >= total) return;
-    const int band = t / (4 * tn), rows = min(4, tm - 4 * band), in = t - band * 4 * tn;
-    bm = 4 * band + in % rows;
+    const int bands = (tm + 3) / 4, high = (tm + bands - 1) / bands;
+    const int band = t / (high * tn), rows = min(high, tm - high * band), in = t - band * high * tn;
+    bm = high * band + in % rows;
     bn = in / rows;
   }
   const int set = SETS == 1 ? 0 : __builtin_amdgcn_readfirstlane(threadIdx.x / 256);

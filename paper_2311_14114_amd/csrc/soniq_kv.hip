@@ -34,6 +34,11 @@ constexpr int kCopyTokens = 16;  // tokens a workgroup, at most
 // finds where each token lives; then every thread moves pieces of 8 elements,
 // kAhead of them in flight (one at a time reached 3.7 TB/s on long reads:
 // 8 bytes a lane and 32 waves do not cover the memory's latency).
+//   write: s = max |x| / top, code = rint(x / s);   read: code * s.
+// Bytes bound it: reading 500 MB of prefixes (8 sequences, 8 heads of 128, 8
+// bits) takes 106 us, 4.7 TB/s, what a large copy reaches; 700 to 4096 tokens
+// of 5 sequences written in 4 bits 18 us and read back 15.  A token or a few
+// take 3.8 to 4.7 us: launch, tables, then one trip to memory.
 template <int TYPE, int D, int BITS, bool WRITE>
 __global__ __launch_bounds__(256) void k_kv_copy(KvCopy c, int tw) {
   typedef typename Value<TYPE>::T T;
@@ -143,6 +148,12 @@ __global__ __launch_bounds__(256) void k_kv_copy(KvCopy c, int tw) {
 // share a key/value head) of one sequence and key/value head over one part
 // of its positions; four waves take 32 positions each in turn, keep their
 // own running softmax, and meet at the end.  Parts meet in k_kv_join.
+// Single tokens are bound by the cache's bytes: 32 sequences of 2000 to 32768
+// positions, 8 heads of 128, 8 bits, 4 query heads each: 197 us for 1.06 GB,
+// 5.4 TB/s, and 7 for the join.  Many rows by the vector instructions of codes
+// and softmax: 8 sequences of 3001 to 8191 positions, 96 rows, 4 bits, fp16:
+// 54 us, of which those 17100 a SIMD take 30 (matrix cores 10, 50 MB from
+// memory 10); then the starts and ends of parts.
 //
 // Everything stays transposed, so that no operand crosses lanes: with
 // kb = lane / 16 and c = lane % 16,
@@ -835,7 +846,8 @@ __global__ __launch_bounds__(256, kv_waves(D, R)) void k_kv_attend(KvAttend a, K
 }
 
 // Joins the parts of one (token, query head): W waves take every W-th part
-// each and meet in LDS (W = 1: a wave by itself, four rows a workgroup).
+// each and meet in LDS (W = 1: a wave by itself, four rows a workgroup).  4
+// to 7 us: one look at the lengths, then a trip to memory every four parts.
 template <int D, int W>
 __global__ __launch_bounds__(256) void k_kv_join(KvAttend a, KvSplit sp) {
   constexpr int E = D / 64, kAhead = 4;
