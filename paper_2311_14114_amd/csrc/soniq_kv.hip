@@ -935,7 +935,11 @@ __global__ __launch_bounds__(256) void k_kv_join(KvAttend a, KvSplit sp) {
 //     96                 65.5                      66            53.5
 // (96 rows, 4 bits, fp16: 61.2, 67.7, 55.6.)
 // More sequences, or few positions: by the longest one's length, about a
-// thousand workgroups.  Four row tiles a wave spill.
+// thousand workgroups.  Up to 512 positions (384 with two row tiles) stay in
+// one part, which needs no second launch (one sequence, 8 heads of 128, 4
+// query heads each, us in a graph: 200 positions 7.5 and 9.0, 384 8.6 and 9.3,
+// 512 9.6 and 9.1, 768 11.4 and 9.6; a launch from Python is 3 more).
+// Four row tiles a wave spill.
 KvSplit kv_split(const KvDims& d, int32_t q_heads, int64_t B, int64_t max_q, int64_t max_kv) {
   const int64_t rows = max_q * (q_heads / d.heads);
   KvSplit s;
@@ -945,7 +949,7 @@ KvSplit kv_split(const KvDims& d, int32_t q_heads, int64_t B, int64_t max_q, int
   auto over = [&](int64_t n) { return (pieces * units + n - 1) / n; };
   const bool by_lengths = B <= 64 && pieces * units > 512;
   const int64_t cap = std::max<int64_t>(8 * s.R, over(8192));
-  const int64_t chunk = std::min(over(1024), cap);
+  const int64_t chunk = pieces <= (s.R == 1 ? 4 : 3) ? pieces : std::min(over(1024), cap);
   const int64_t parts = std::min((pieces + chunk - 1) / chunk, std::max<int64_t>(((int64_t)1 << 22) / units, 1));
   s.chunk = (int)chunk;
   s.parts = (int)parts;
