@@ -4,7 +4,7 @@
 //   s_a[m] = max_k |A[m,k]| / 127,  Qa = rint(A / s_a).
 //
 //   k_rows       codes and scales of rows, one wave or one workgroup a row
-//   k_i8_fused   one to four tokens, quantized where they are used: one launch
+//   k_i8_fused   up to 16 short tokens, quantized where they are used: one launch
 //   k_i8_skinny  up to 64 tokens: bound by the weights' bytes; the waves of a
 //                workgroup split K, each with its own part of LDS
 //   k_i8_tile    more tokens: bound by LDS where tiles are few and small, by
@@ -244,22 +244,26 @@ __global__ __launch_bounds__(512) void k_i8_skinny(I8Gemm g) {
   }
 }
 
-// One to four tokens with their quantization in the same launch: every
-// workgroup makes the codes for itself (at most kFusedMost elements, 32 a
-// thread), in LDS, while its first weights are on their way.  16 output
-// channels a workgroup, K over the waves as above.  1 x 4096 x 4096 takes
-// 6.1 us: 17 MB at 2.8 TB/s, half of it the way from the launch to the codes.
-constexpr int kFusedMost = 16384;
+// Up to 16 tokens with their quantization in the same launch: every workgroup
+// makes the codes for itself (at most kFusedMost elements, 32 a thread), in
+// LDS, while its first weights are on their way.  16 output channels a
+// workgroup, K over the waves as above, U segments of each in flight.
+// 1 x 4096 x 4096 takes 6.1 us: 17 MB at 2.8 TB/s, half of it the way from the
+// launch to the codes.  Past 16384 elements the codes cost every workgroup more
+// than a launch of their own (8 x 4096 x 4096: 14.9 us in a graph, 10.5 with
+// two launches); from 8192 on they are level (16 x 2304 x 768: 7.4 and 7.0),
+// and a launch from Python is 4 more.
+constexpr int kFusedRows = 16, kFusedMost = 16384;
 
-template <int TYPE>
-__global__ __launch_bounds__(512) void k_i8_fused(I8Gemm g, const typename Value<TYPE>::T* A, int64_t lda) {
-  constexpr int U = 4, kPad = 144, kHeld = kFusedMost / (8 * 512);
+template <int TYPE, int U>
+__global__ __launch_bounds__(512, U == 2 ? 6 : 4) void k_i8_fused(I8Gemm g, const typename Value<TYPE>::T* A, int64_t lda) {
+  constexpr int kPad = 144, kHeld = kFusedMost / (8 * 512);
   // codes of token m at m * (K up to a multiple of 128 + 16), then the waves'
   // weights (later the sums), then the largest |x| and the scale of each token
-  __shared__ __align__(16) int8_t codes[kFusedMost + 4 * kPad];
+  __shared__ __align__(16) int8_t codes[kFusedMost + kFusedRows * kPad];
   __shared__ __align__(16) int8_t wlds[8 * 2048];
-  __shared__ uint32_t amax[4];
-  __shared__ float sa[4];
+  __shared__ uint32_t amax[kFusedRows];
+  __shared__ float sa[kFusedRows];
   const int tid = threadIdx.x, lane = tid % 64, r = lane % 16, q = lane / 16;
   const int wave = __builtin_amdgcn_readfirstlane(tid / 64);
   const int M = (int)g.M, K = (int)g.K, nv = (K + 7) / 8, pitch = (K + 127) / 128 * 128 + 16;
@@ -286,7 +290,7 @@ __global__ __launch_bounds__(512) void k_i8_fused(I8Gemm g, const typename Value
 #pragma unroll
       for (int i = 0; i < 2; ++i) w[u][i] = load16(row[i] + (wave + 8 * u) * 128 + 16 * lc);
     }
-  if (tid < 4) amax[tid] = 0;
+  if (tid < kFusedRows) amax[tid] = 0;
   lds_barrier();
 #pragma unroll
   for (int i = 0; i < kHeld; ++i) {
@@ -353,18 +357,16 @@ __global__ __launch_bounds__(512) void k_i8_fused(I8Gemm g, const typename Value
     mma(full);
   }
   __syncthreads();
-  int* red = reinterpret_cast<int*>(wlds);  // [wave][e][column]: tokens 0 .. 3 are in the first 16 lanes
-  if (q == 0) {
+  int* red = reinterpret_cast<int*>(wlds);  // [wave][token][column]
 #pragma unroll
-    for (int e = 0; e < 4; ++e) red[(wave * 4 + e) * 16 + r] = acc[e];
-  }
+  for (int e = 0; e < 4; ++e) red[(wave * 16 + 4 * q + e) * 16 + r] = acc[e];
   __syncthreads();
   const int64_t n = n0 + tid % 16;
   if (tid < 16 * M && n < g.N) {
     const int m = tid / 16;
     int sum = 0;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) sum += red[(i * 4 + m) * 16 + tid % 16];
+    for (int i = 0; i < 8; ++i) sum += red[(i * 16 + m) * 16 + tid % 16];
     float v = scaled(sum, sa[m], g.sw[n]);
     if (g.bias) v = __fadd_rn(v, g.bias[n]);
     store_y(g, m * g.ldy + n, v);
@@ -746,10 +748,16 @@ void launch_skinny(const I8Gemm& g, hipStream_t stream) {
     k_i8_skinny<A8, 3><<<(unsigned)((g.N + 47) / 48), 512, 0, stream>>>(g);
 }
 
+// Four segments in flight leave two workgroups a CU their registers, two
+// segments three, which more than two a CU gain from (us in a graph, four and
+// two: 1 x 11008 x 4096 14.0 and 12.4, 2 x 11008 x 8192 24.6 and 20.8, but
+// 1 x 4096 x 4096 8.2 and 8.6, 4 x 4096 x 4096 10.4 and 11.0).
 template <int TYPE>
 void launch_fused(const I8Gemm& g, const void* A, int64_t lda, hipStream_t stream) {
   const auto* a = static_cast<const typename Value<TYPE>::T*>(A);
-  k_i8_fused<TYPE><<<(unsigned)((g.N + 15) / 16), 512, 0, stream>>>(g, a, lda);
+  const unsigned grid = (unsigned)((g.N + 15) / 16);
+  if (grid <= 512) k_i8_fused<TYPE, 4><<<grid, 512, 0, stream>>>(g, a, lda);
+  else k_i8_fused<TYPE, 2><<<grid, 512, 0, stream>>>(g, a, lda);
 }
 
 }  // namespace
@@ -762,7 +770,7 @@ hipError_t launch_quantize_rows(const void* A, int a_type, int64_t M, int64_t K,
   return hipGetLastError();
 }
 
-bool i8_fused(int64_t M, int64_t K) { return M <= 4 && M * ((K + 7) / 8 * 8) <= kFusedMost; }
+bool i8_fused(int64_t M, int64_t K) { return M <= kFusedRows && M * ((K + 7) / 8 * 8) <= kFusedMost; }
 
 hipError_t launch_i8_fused(const I8Gemm& g, const void* A, int a_type, int64_t lda, hipStream_t stream) {
   if (a_type == SONIQ_F32) launch_fused<SONIQ_F32>(g, A, lda, stream);

@@ -119,7 +119,9 @@ def test_i8_gemm(M, N, K, form):
                                        (4, 256, 2048, 0), (5, 64, 512, 0), (8, 130, 11008, 0), (9, 40, 65, 0),
                                        (40, 300, 1024, 5), (300, 512, 640, 0), (1, 24, 65536, 0),
                                        (1, 100, 1, 0), (1, 70, 16384, 0), (1, 70, 16385, 1), (2, 40, 8192, 0), (2, 40, 513, 7),
-                                       (3, 129, 63, 0), (4, 16, 4089, 0), (4, 16, 4097, 0), (4, 5000, 127, 2), (55, 8200, 300, 0)])
+                                       (3, 129, 63, 0), (4, 16, 4089, 0), (4, 16, 4097, 0), (4, 5000, 127, 2), (55, 8200, 300, 0), (16, 70, 1024, 0),
+                                       (16, 70, 1025, 1), (13, 8300, 1257, 3), (2, 8300, 8192, 0), (16, 8200, 129, 0),
+                                       (7, 33, 2336, 0), (15, 31, 65, 2), (17, 40, 64, 0), (11, 9000, 7, 1)])
 @pytest.mark.parametrize("dtype", ["fp32", "bf16", "fp16"])
 def test_quantize_i8_gemm_equals_the_two_calls(M, N, K, gap, dtype):
     A = _tokens(M, K, dtype, gap)
@@ -231,7 +233,7 @@ def test_binding_refusals():
            (TypeError, lambda: sq.soniq_quantize_i8_gemm(x, W, sw.cpu())),
            (TypeError, lambda: sq.soniq_quantize_i8_gemm(x, W, sw, dtype=torch.float64)),
            (ValueError, lambda: sq.soniq_quantize_i8_gemm(x, W, sw, out=torch.empty((4, 21), device="cuda"))),
-           (sq.SoniqError, lambda: sq.soniq_quantize_i8_gemm(torch.randn((9, 64), device="cuda"), W, sw,
+           (sq.SoniqError, lambda: sq.soniq_quantize_i8_gemm(torch.randn((17, 64), device="cuda"), W, sw,
                                                              work=torch.empty(16, dtype=torch.uint8, device="cuda"))),
            (TypeError, lambda: sq.soniq_i8_gemm(x, sw, W, sw))]
     for error, call in bad:

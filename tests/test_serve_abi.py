@@ -33,7 +33,7 @@ def _with(base, **changes):
 ROWS = dict(A=FAKE, type=0, M=4, K=32, lda=32, Q=FAKE, ldq=32, s=FAKE, stream=None)
 GEMM = dict(A=FAKE, lda=32, s_a=FAKE, W=FAKE, ldw=32, s_w=FAKE, bias=None, M=4, N=8, K=32, Y=FAKE, y_type=1, ldy=8,
             stream=None)
-BOTH = dict(A=FAKE, type=0, lda=32, W=FAKE, ldw=32, s_w=FAKE, bias=None, M=6, N=8, K=32, Y=FAKE, y_type=1, ldy=8,
+BOTH = dict(A=FAKE, type=0, lda=32, W=FAKE, ldw=32, s_w=FAKE, bias=None, M=20, N=8, K=32, Y=FAKE, y_type=1, ldy=8,
             work=FAKE, bytes=1 << 20, stream=None)
 
 
@@ -51,7 +51,7 @@ BOTH = dict(A=FAKE, type=0, lda=32, W=FAKE, ldw=32, s_w=FAKE, bias=None, M=6, N=
     ("gemm", GEMM, dict(K=70000, lda=70000, ldw=70000), UNSUP), ("gemm", GEMM, dict(N=1 << 31, ldy=1 << 31), UNSUP),
     ("gemm", GEMM, dict(M=(1 << 30) - 64), UNSUP), ("gemm", GEMM, dict(M=1 << 16, N=1 << 20, ldy=1 << 20), UNSUP),
     ("both", BOTH, dict(A=None), BAD), ("both", BOTH, dict(W=None), BAD), ("both", BOTH, dict(work=None), BAD),
-    ("both", BOTH, dict(work=FAKE + 8), BAD), ("both", BOTH, dict(bytes=6 * 32 + 23), BAD),
+    ("both", BOTH, dict(work=FAKE + 8), BAD), ("both", BOTH, dict(bytes=20 * 32 + 79), BAD),
     ("both", BOTH, dict(lda=31), BAD), ("both", BOTH, dict(y_type=9), BAD)],
     ids=lambda v: str(v) if isinstance(v, (str, int)) else "-".join(v) if isinstance(v, dict) and len(v) < 4 else "")
 def test_linear_refusals(L, fn, base, changes, status):
@@ -128,10 +128,11 @@ def test_nothing_to_do_is_ok(L):
 
 def test_workspaces(L):
     n = ctypes.c_int64(-1)
-    assert L.soniq_quantize_i8_gemm_workspace(5, 100, ctypes.byref(n)) == 0
-    assert n.value >= 5 * 100 + 5 * 4
-    for few in (0, 1, 4):                             # quantized where they are used
-        assert L.soniq_quantize_i8_gemm_workspace(few, 100, ctypes.byref(n)) == 0 and n.value == 0
+    for M, K in ((17, 100), (16, 1025), (1, 16385)):
+        assert L.soniq_quantize_i8_gemm_workspace(M, K, ctypes.byref(n)) == 0
+        assert n.value >= M * K + M * 4
+    for M, K in ((0, 100), (1, 16384), (4, 100), (16, 1024)):  # quantized where they are used
+        assert L.soniq_quantize_i8_gemm_workspace(M, K, ctypes.byref(n)) == 0 and n.value == 0
     for bad in ((-1, 4), (4, 0)):
         assert L.soniq_quantize_i8_gemm_workspace(*bad, ctypes.byref(n)) == BAD
     assert L.soniq_quantize_i8_gemm_workspace(4, 4, None) == BAD
