@@ -946,7 +946,7 @@ KvSplit kv_split(const KvDims& d, int32_t q_heads, int64_t B, int64_t max_q, int
   s.R = rows <= 16 ? 1 : 2;
   s.RB = (int)((rows + 16 * s.R - 1) / (16 * s.R));
   const int64_t units = B * d.heads * s.RB, pieces = max_kv < 1 ? 1 : (max_kv + 127) / 128;
-  auto over = [&](int64_t n) { return (pieces * units + n - 1) / n; };
+  auto over = [&](int64_t n) { return std::min((pieces * units + n - 1) / n, (int64_t)1 << 24); };
   const bool by_lengths = B <= 64 && pieces * units > 512;
   const int64_t cap = std::max<int64_t>(8 * s.R, over(8192));
   const int64_t chunk = pieces <= (s.R == 1 ? 4 : 3) ? pieces : std::min(over(1024), cap);
@@ -956,7 +956,7 @@ KvSplit kv_split(const KvDims& d, int32_t q_heads, int64_t B, int64_t max_q, int
   s.cap = by_lengths && parts > 1 ? (int)cap : 0;
   s.per = 256.0f / ((float)d.heads * (float)s.RB);
   s.waves = kv_waves(d.head_dim, s.R);
-  s.pad = s.R == 2 && s.waves > 2 && by_lengths && over(3 * 256) <= 9;
+  s.pad = s.R == 2 && s.waves > 2 && s.cap && over(3 * 256) <= 9;
   if (s.pad) s.waves = 2;
   s.least = s.R == 2 ? s.waves : 2;
   return s;

@@ -267,6 +267,22 @@ def test_parts_of_very_different_lengths(B, longest, rows, max_kv):
     _check_attention(cache, h, q, table, cu, lens, 4, max_q=rows, max_kv=max_kv)
 
 
+def test_the_most_sequences_with_the_longest_hint():
+    """65535 sequences of 32 heads, told to hold 2^31 - 1 positions: the cut's
+    arithmetic stays in range, and empty ones among them stay empty."""
+    r = np.random.default_rng(25)
+    B = 65535
+    cache, h = _random_cache(r, 3, 16, 32, 64, 8)
+    table = np.full((B, 2), -1, np.int32)
+    table[0], table[B - 1] = [1, 0], [2, -1]
+    lens = np.zeros(B, np.int32)
+    lens[0], lens[B - 1] = 20, 9
+    cu = np.zeros(B + 1, np.int32)
+    cu[1:], cu[40000:], cu[B] = 1, 2, 3               # sequence 39999 has a new token and no position
+    q = torch.from_numpy(r.standard_normal((4, 32, 64)).astype(np.float32)).to(torch.bfloat16).cuda()
+    _check_attention(cache, h, q, table, cu, lens, 8, max_q=1, max_kv=2**31 - 1)
+
+
 def test_two_graphs_share_a_workspace():
     """Two layers' attention captured on one workspace, replayed in turn, with
     eager work on it between the replays."""
