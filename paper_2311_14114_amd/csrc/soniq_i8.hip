@@ -75,21 +75,21 @@ __device__ __forceinline__ uint32_t wave_max(uint32_t m) {
   return m;
 }
 
-// T threads a row, 256 a workgroup.  A row of up to 8 * T * kHeld elements
-// stays in registers between its maximum and its codes; longer ones are read
-// again for the rest.  Bytes bound it where rows are many: 4096 x 11008 bf16
-// take 34 us, 136 MB at 4.0 TB/s (a large copy reaches 4.8; the part of a row
-// past the 8192 held elements comes from L2); 8192 x 8192 51 us, 202 MB at
-// 4.0.  Few rows take two dependent trips to memory and a barrier: 40 x 4096
-// 4.3 us.
-template <int TYPE, int T>
-__global__ __launch_bounds__(256) void k_rows(const typename Value<TYPE>::T* A, int64_t M, int K, int64_t lda,
-                                              int8_t* Q, int64_t ldq, float* s) {
-  constexpr int kHeld = 4;
-  __shared__ uint32_t part[4];
+// T threads a row: a wave, four of them a workgroup, or a workgroup.  A row of
+// up to 8 * T * kHeld elements stays in registers between its maximum and its
+// codes; longer ones are read again for the rest.  Bytes bound it where rows
+// are many: 8192 x 8192 bf16 take 48 us, 202 MB at 4.2 TB/s (a large copy
+// reaches 4.8), 4096 x 4096 13.3, 50 MB at 3.8.  Few rows take two dependent
+// trips to memory and a barrier: 40 x 4096 4.3 us.
+template <int TYPE, int T, int kHeld>
+__global__ __launch_bounds__(T < 256 ? 256 : T) void k_rows(const typename Value<TYPE>::T* A, int64_t M, int K,
+                                                            int64_t lda, int8_t* Q, int64_t ldq, float* s) {
+  static_assert(T == 64 || T >= 256, "a row is a wave's or a workgroup's");
+  constexpr int kRows = T < 256 ? 256 / T : 1;  // a workgroup
+  __shared__ uint32_t part[T / 64];
   const int t = threadIdx.x % T;
-  const int64_t step = (int64_t)gridDim.x * (256 / T);
-  for (int64_t m = (int64_t)blockIdx.x * (256 / T) + threadIdx.x / T; m < M; m += step) {
+  const int64_t step = (int64_t)gridDim.x * kRows;
+  for (int64_t m = (int64_t)blockIdx.x * kRows + threadIdx.x / T; m < M; m += step) {
     const typename Value<TYPE>::T* a = A + m * lda;
     Eight<TYPE> x[kHeld];
 #pragma unroll
@@ -103,11 +103,12 @@ __global__ __launch_bounds__(256) void k_rows(const typename Value<TYPE>::T* A, 
       mx = max(mx, y.amax());
     }
     mx = wave_max(mx);
-    if constexpr (T == 256) {
+    if constexpr (T > 64) {
       __syncthreads();  // the last row's maxima have been read
       if (threadIdx.x % 64 == 0) part[threadIdx.x / 64] = mx;
       __syncthreads();
-      mx = max(max(part[0], part[1]), max(part[2], part[3]));
+#pragma unroll
+      for (int w = 0; w < T / 64; ++w) mx = max(mx, part[w]);
     }
     const RowCoder rc(mx, 127.0f);
     if (t == 0) s[m] = rc.s;
@@ -678,17 +679,36 @@ __global__ __launch_bounds__(256) void k_i8_short(I8Gemm g) {
   }
 }
 
+// Threads a row and pieces of 8 elements that each holds: as few as hold the
+// row, since a piece past its end still costs its checks and registers, and
+// registers cost waves; two a thread keep enough loads in flight.  us in a
+// graph, 16-bit rows, and what 256 threads of four pieces (a wave of four up to
+// 2048 elements) take:
+//   8192 x  300  64, 1:  6.6   9.7     4096 x  6000  256, 3: 16.7  20.2
+//   8192 x 1024  64, 2:  9.2  10.8     8192 x  8192  512, 2: 47.7  50.9
+//    300 x 2048 256, 1:  4.3   5.5     4096 x 11008  768, 2: 39.7  40.7
+//   4096 x 2560 256, 2: 11.7  17.7     4096 x 14336  768, 3: 46.7  49.3
+//   4096 x 4096 256, 2: 13.3  18.3     2000 x 20000  768, 3: 30.1  37.3
 template <int TYPE>
 void launch_rows(const void* A, int64_t M, int64_t K, int64_t lda, int8_t* Q, int64_t ldq, float* s,
                  hipStream_t stream) {
   const auto* a = static_cast<const typename Value<TYPE>::T*>(A);
-  if (K <= 2048 && M > 256) {
-    const unsigned grid = (unsigned)std::min<int64_t>((M + 3) / 4, 1 << 20);
-    k_rows<TYPE, 64><<<grid, 256, 0, stream>>>(a, M, (int)K, lda, Q, ldq, s);
-  } else {
-    const unsigned grid = (unsigned)std::min<int64_t>(M, 1 << 20);
-    k_rows<TYPE, 256><<<grid, 256, 0, stream>>>(a, M, (int)K, lda, Q, ldq, s);
-  }
+  auto go = [&](auto threads, auto held) {
+    constexpr int T = decltype(threads)::value, kRows = T < 256 ? 256 / T : 1;
+    const unsigned grid = (unsigned)std::min<int64_t>((M + kRows - 1) / kRows, 1 << 20);
+    k_rows<TYPE, T, decltype(held)::value><<<grid, T < 256 ? 256 : T, 0, stream>>>(a, M, (int)K, lda, Q, ldq, s);
+  };
+#define GO(T, H) go(std::integral_constant<int, T>(), std::integral_constant<int, H>())
+  if (K <= 512 && M > 256) GO(64, 1);
+  else if (K <= 1024 && M > 256) GO(64, 2);
+  else if (K <= 2048 && M > 1024) GO(64, 4);
+  else if (K <= 2048) GO(256, 1);
+  else if (K <= 4096) GO(256, 2);
+  else if (K <= 6144) GO(256, 3);
+  else if (K <= 8192) GO(512, 2);
+  else if (K <= 12288) GO(768, 2);
+  else GO(768, 3);
+#undef GO
 }
 
 template <int BM, int BN, bool CLAMP = false, int SETS = 1>

@@ -46,7 +46,10 @@ def _same(got, want):
 @pytest.mark.parametrize("dtype", ["fp32", "bf16", "fp16"])
 @pytest.mark.parametrize("M,K,gap,offset", [
     (1, 1, 0, 0), (1, 64, 0, 0), (3, 100, 5, 1), (5, 4091, 3, 3), (2, 4096, 0, 0), (33, 768, 0, 2),
-    (700, 130, 1, 0), (9, 8192, 8, 0), (2, 16389, 0, 0), (1, 65536, 0, 1), (4100, 16, 0, 0)])
+    (700, 130, 1, 0), (9, 8192, 8, 0), (2, 16389, 0, 0), (1, 65536, 0, 1), (4100, 16, 0, 0),
+    (300, 512, 0, 0), (257, 513, 1, 0), (300, 1024, 0, 1), (260, 1025, 0, 0), (1025, 1025, 0, 0), (1030, 2048, 0, 0),
+    (300, 2048, 0, 0), (3, 2049, 0, 0), (3, 4097, 1, 0), (3, 6144, 0, 0), (3, 6145, 0, 0), (2, 8193, 0, 1), (3, 12288, 0, 0),
+    (2, 12289, 0, 0), (2, 18432, 0, 0), (2, 18437, 0, 0)])
 def test_quantize_rows(M, K, gap, offset, dtype):
     A = _tokens(M, K, dtype, gap, offset=offset)
     print(f"[gpu] quantize_rows {M}x{K} {dtype}", flush=True)
@@ -56,6 +59,18 @@ def test_quantize_rows(M, K, gap, offset, dtype):
     _same(Q, torch.from_numpy(q))
     _same(s, torch.from_numpy(sc))
     assert bool((back[:, K:] == 99).all())          # columns past K are left alone
+
+
+def test_more_rows_than_workgroups():
+    """Past 2^20 workgroups each takes several rows."""
+    M, K = (1 << 20) + 300, 2056
+    A = torch.randn((4096, K), device="cuda").to(torch.bfloat16).repeat(M // 4096 + 1, 1)[:M]
+    A[(1 << 20):] *= 3
+    print("[gpu] rows past 2^20", flush=True)
+    Q, s = sq.soniq_quantize_rows(A)
+    for part in (slice(0, 300), slice(M - 700, M)):
+        q, t = sq.soniq_quantize_rows(A[part])
+        assert torch.equal(Q[part], q) and torch.equal(s[part], t)
 
 
 def test_quantize_rows_special():
