@@ -98,15 +98,17 @@ def kv_read(codes, scales, table, cu, start, bits):
     return np.concatenate(out)
 
 
-def attention(q, kc, ks, vc, vs, table, cu, kv_len, bits, scale, mask=None):
+def attention(q, kc, ks, vc, vs, table, cu, kv_len, bits, scale, mask=None, weight=2.0**-11, exact_sums=False):
     """float64 attention of q [T, Hq, D] over the cache.  Returns (out, lse,
-    bound): bound is what half a step of fp16 in the softmax weights and fp32
-    sums can move an output by, before its own rounding:
-      - a weight held in fp16 is off by at most 2^-11 of itself, or by 2^-25
-        of the largest weight where it is subnormal;
+    bound): bound is what rounding the softmax weights and fp32 sums can move
+    an output by, before its own rounding:
+      - a weight is off by at most `weight` of itself (2^-11: one fp16
+        number), or by 2^-25 of the largest weight where it is subnormal;
       - a score is off by (D + 16) roundings of 2^-24 of sum |q k| (and of
         its own size for the scalings and the exponent), which moves a weight
         by that much, relatively, in the numerator and in the sum;
+        exact_sums: q and codes are integers whose sums fp32 holds, in any
+        order, so that only the roundings of the scalings are left;
       - sums of n terms in fp32 add n roundings of 2^-24."""
     T, Hq, D = q.shape
     P, H, S, _ = kc.shape
@@ -146,10 +148,12 @@ def attention(q, kc, ks, vc, vs, table, cu, kv_len, bits, scale, mask=None):
                         out[t, h * G + g] = p @ V
                         lse[t, h * G + g] = m + np.log(e.sum())
                         size = abs(scale) * (np.abs(K) @ np.abs(x))
-                        ds = (D + 16) * 2.0**-24 * size.max() + 8 * 2.0**-24 * (1 + np.abs(z).max())
-                        # the fp16 grid of q: relative to the row's largest element
-                        ds += abs(scale) * 2.0**-24 * np.abs(x).max(initial=0) * np.abs(K).sum(1).max()
+                        ds = 8 * 2.0**-24 * (1 + np.abs(z).max())
+                        if not exact_sums:
+                            ds += (D + 16) * 2.0**-24 * size.max()
+                            # the fp16 grid of q: relative to the row's largest element
+                            ds += abs(scale) * 2.0**-24 * np.abs(x).max(initial=0) * np.abs(K).sum(1).max()
                         A = p @ np.abs(V)
                         top = (p * sv[seen, h]).max() * np.abs(cv[seen, h]).sum(0)
-                        bound[t, h * G + g] = A * (2.0**-11 + 2 * ds + len(z) * 2.0**-24) + 2.0**-25 * top
+                        bound[t, h * G + g] = A * (weight + 2 * ds + len(z) * 2.0**-24) + 2.0**-25 * top
     return out, lse, bound
