@@ -184,10 +184,13 @@ __global__ __launch_bounds__(256) void k_kv_copy(KvCopy c, int tw) {
 // 2^8 (fp16 has room) or an exponential nears fp32's end.  So a weight is off
 // by at most half a step of fp16 whatever the range of the V scales, down to
 // s_v = 2^-60 of the row's largest exp2(s - r), and rescaling is rare.
-// Half a step of fp16 in each weight is an eighth of a bf16 output's own, but
-// as much as an fp16 output's: for those (FINE) a second product takes what
-// the rounding left (without it, their error against 64 bits was 1.4 to 1.5
-// times that of rounding the exact output).
+// Half a step of fp16 in each weight is as much as an fp16 output's own and an
+// eighth of a bf16 output's, so a second product takes what the rounding left
+// (without it, fp16 outputs' error against 64 bits was 1.4 to 1.5 times that of
+// rounding the exact output).  It costs single tokens nothing to speak of (201
+// us and 201 for 32 sequences of 2000 to 32768 positions, bf16), many rows 3 to
+// 9% (8 sequences of 3001 to 8191 positions, 96 rows, 8 bits, bf16: 52.4 and
+// 57.1).
 typedef _Float16 h2 __attribute__((ext_vector_type(2)));
 typedef _Float16 h8 __attribute__((ext_vector_type(8)));
 typedef float f4 __attribute__((ext_vector_type(4)));
@@ -634,7 +637,7 @@ constexpr int kv_waves(int D, int R) {
   return D * R <= 64 ? 5 : D * R <= 128 ? 4 : D * R <= 192 || D == 128 ? 3 : 2;
 }
 
-template <int D, int BITS, int R, bool FINE>
+template <int D, int BITS, int R>
 __global__ __launch_bounds__(256, kv_waves(D, R)) void k_kv_attend(KvAttend a, KvSplit sp) {
   constexpr int RB = D * BITS / 8;   // bytes of a cache row
   constexpr int KB = RB / 4, VB = RB / 16;
@@ -732,7 +735,7 @@ __global__ __launch_bounds__(256, kv_waves(D, R)) void k_kv_attend(KvAttend a, K
       const uint32_t valid = __builtin_amdgcn_readfirstlane(L.p.valid[st]);
       const int64_t j0 = (int64_t)p0 + st * 32 - base;
       const bool whole = valid == ~0u && j0 <= -32;
-      h8 P[R], fine[FINE ? R : 1];
+      h8 P[R], fine[R];
 #pragma unroll
       for (int rt = 0; rt < R; ++rt) {
         if constexpr (R > 1) __builtin_amdgcn_sched_barrier(0);
@@ -761,11 +764,7 @@ __global__ __launch_bounds__(256, kv_waves(D, R)) void k_kv_attend(KvAttend a, K
 #pragma unroll
           for (int j = 0; j < DB; ++j) O[rt][j] *= f;
         });
-        if constexpr (FINE) weigh_fine(s, P[rt], fine[rt]);
-        else {
-#pragma unroll
-          for (int e = 0; e < 8; ++e) P[rt][e] = (_Float16)s[e];
-        }
+        weigh_fine(s, P[rt], fine[rt]);
       }
 
       // O^T += V^T P^T, one element of d per lane column at a time
@@ -778,7 +777,7 @@ __global__ __launch_bounds__(256, kv_waves(D, R)) void k_kv_attend(KvAttend a, K
 #pragma unroll
         for (int rt = 0; rt < R; ++rt) {
           O[rt][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(x, P[rt], O[rt][j], 0, 0, 0);
-          if constexpr (FINE) O[rt][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(x, fine[rt], O[rt][j], 0, 0, 0);
+          O[rt][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(x, fine[rt], O[rt][j], 0, 0, 0);
         }
       }
       if (more) load_v(st + 4);
@@ -968,13 +967,8 @@ void launch_attend(const KvAttend& a, const KvSplit& s, hipStream_t stream) {
   const dim3 grid((unsigned)((u + 7) / 8 * 8 * s.RB)), block(256);
   constexpr size_t kTwo = 56 << 10;  // of 160 KB
   const size_t pad = s.pad ? kTwo - std::min(kTwo, kv_lds<D, 2>()) : 0;
-  if (a.type == SONIQ_F16) {
-    if (s.R == 1) k_kv_attend<D, BITS, 1, true><<<grid, block, 0, stream>>>(a, s);
-    else k_kv_attend<D, BITS, 2, true><<<grid, block, pad, stream>>>(a, s);
-  } else {
-    if (s.R == 1) k_kv_attend<D, BITS, 1, false><<<grid, block, 0, stream>>>(a, s);
-    else k_kv_attend<D, BITS, 2, false><<<grid, block, pad, stream>>>(a, s);
-  }
+  if (s.R == 1) k_kv_attend<D, BITS, 1><<<grid, block, 0, stream>>>(a, s);
+  else k_kv_attend<D, BITS, 2><<<grid, block, pad, stream>>>(a, s);
   if (s.parts <= 1) return;
   const int64_t x = (int64_t)a.T * a.q_heads;
   // a wave a row, or four where rows are few and parts many (16 sequences of
