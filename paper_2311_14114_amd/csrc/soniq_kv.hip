@@ -176,14 +176,14 @@ __global__ __launch_bounds__(256) void k_kv_copy(KvCopy c, int tw) {
 // (bf16 queries are exact in it down to 2^-22 of the row's largest element,
 // the sixteenths that meet odd 4-bit codes too).
 //
-// Softmax of a row over the positions so far, all in fp32 and base 2, has one
-// reference r for the sum and the weights:
-//   l = sum exp2(s - r),  w = exp2(s - r) * s_v,  outputs = sum w * code.
-// w is rounded to fp16 for the product, so r is chosen by the weights: the
-// largest w so far is near 1 (`ref`), and r moves only when one passes it by
-// 2^8 (fp16 has room) or an exponential nears fp32's end.  So a weight is off
-// by at most half a step of fp16 whatever the range of the V scales, down to
-// s_v = 2^-60 of the row's largest exp2(s - r), and rescaling is rare.
+// Softmax of a row over the positions so far, all in fp32 and base 2:
+//   p = exp2(s - r),  l = sum p,  w = p * s_v,  outputs = sum w * code.
+// The reference r has to do with scores alone: one that was met, so that l
+// neither overflows nor vanishes.  It moves only where a p passes 2^80.  The
+// weights go into the product as fp16, in a unit of their own, a power of two
+// that follows the largest w so far (between 2^6 and 2^14 units of it): only
+// exponents change with it, so that scores and V scales may rise and fall
+// against each other over all of fp32's range.  Both are rarely moved.
 // Half a step of fp16 in each weight is as much as an fp16 output's own and an
 // eighth of a bf16 output's, so a second product takes what the rounding left
 // (without it, fp16 outputs' error against 64 bits was 1.4 to 1.5 times that of
@@ -220,10 +220,15 @@ __device__ __forceinline__ float quad_sum(float x) {
 // the weights in x, and calls scale(f) where the outputs so far have to be
 // multiplied.  A row starts at r = kHidden, where a visible score's exponential
 // is infinite and a hidden one's 0, and stays there while it sees nothing.
-constexpr float kHidden = -3e38f;
+constexpr float kHidden = -3.402823466e38f;
 struct RowSoftmax {
-  float r, l, ref;
+  float r, l;
+  float limit;  // 2^14 units of the weights; a power of two
+  __device__ __forceinline__ static int exponent(float x) { return (int)(__float_as_uint(x) >> 23) - 127; }
+  __device__ __forceinline__ static float power(int e) { return __uint_as_float((uint32_t)(e + 127) << 23); }
+  __device__ __forceinline__ float per_weight() const { return power(14 - exponent(limit)); }  // units in 1
 };
+constexpr float kFirstLimit = 0x1p-112f;  // units in 1: 2^126
 template <int N, class Scale>
 __device__ __forceinline__ void softmax_step(float (&x)[N], const float (&v)[N], float qf, RowSoftmax& st, Scale scale) {
   float w[N], lt, top;
@@ -238,7 +243,7 @@ __device__ __forceinline__ void softmax_step(float (&x)[N], const float (&v)[N],
     }
   };
   weigh();
-  if (__any(lt > 0x1p80f || top > 256.0f * st.ref)) {
+  if (__any(lt > 0x1p80f || top > st.limit)) {
     float mx = x[0];
 #pragma unroll
     for (int e = 1; e < N; ++e) mx = fmaxf(mx, x[e]);
@@ -249,38 +254,33 @@ __device__ __forceinline__ void softmax_step(float (&x)[N], const float (&v)[N],
       st.r = mx;
     }
     weigh();
+    const int was = RowSoftmax::exponent(st.limit) - 8;  // of the largest weight when the unit was chosen
+    int e = was;
     top = quad_max(top);
-    float up = 1.0f;
-    if (top > 256.0f * (st.ref * f)) {
-      const int e = max((int)(__float_as_uint(top) >> 23) - 127, -60);
-      up = __uint_as_float((uint32_t)(127 - min(e, 126)) << 23);
-      st.r += (float)min(e, 126);
-      st.ref = top * up;
-    } else {
-      st.ref *= f;
+    if (f != 1.0f || top > st.limit) {
+      e = min(max(RowSoftmax::exponent(fmaxf(ldexpf(f, was), top)), -120), 119);
+      st.limit = RowSoftmax::power(e + 8);
     }
-    st.l *= f * up;
-    lt *= up;
-#pragma unroll
-    for (int e = 0; e < N; ++e) w[e] *= up;
-    scale(f * up);
+    st.l *= f;
+    scale(ldexpf(f, was - e));
   }
   st.l += lt;
 #pragma unroll
   for (int e = 0; e < N; ++e) x[e] = w[e];
 }
 
-// Weights as fp16 and what that left of them.  Both are cut, not rounded: the
-// second takes up what the first cuts, and itself cuts less than 2^-20 of the
-// weight.
-__device__ __forceinline__ void weigh_fine(const float (&w)[8], h8& coarse, h8& fine) {
+// Weights in their unit as fp16, and what the rounding left of them, cut: 2^-21
+// of the weight at most, or 2^-24 of a unit.
+__device__ __forceinline__ void weigh_fine(const float (&w)[8], float units, h8& coarse, h8& fine) {
   union { h2 p[4]; h8 v; } a, b;
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
-    a.p[i] = __builtin_bit_cast(h2, __builtin_amdgcn_cvt_pkrtz(w[2 * i], w[2 * i + 1]));
-    float lo, hi;  // w - a, exact: one instruction from the fp16 half
-    asm("v_fma_mix_f32 %0, %1, -1.0, %2 op_sel_hi:[1,0,0]" : "=v"(lo) : "v"(a.p[i]), "v"(w[2 * i]));
-    asm("v_fma_mix_f32 %0, %1, -1.0, %2 op_sel:[1,0,0] op_sel_hi:[1,0,0]" : "=v"(hi) : "v"(a.p[i]), "v"(w[2 * i + 1]));
+    asm("v_fma_mixlo_f16 %0, %1, %2, 0" : "=v"(a.p[i]) : "v"(w[2 * i]), "v"(units));
+    asm("v_fma_mixhi_f16 %0, %1, %2, 0" : "+v"(a.p[i]) : "v"(w[2 * i + 1]), "v"(units));
+    float lo, hi;  // w * units - a, exact
+    asm("v_fma_mix_f32 %0, %1, %2, -%3 op_sel_hi:[0,0,1]" : "=v"(lo) : "v"(w[2 * i]), "v"(units), "v"(a.p[i]));
+    asm("v_fma_mix_f32 %0, %1, %2, -%3 op_sel:[0,0,1] op_sel_hi:[0,0,1]"
+        : "=v"(hi) : "v"(w[2 * i + 1]), "v"(units), "v"(a.p[i]));
     b.p[i] = __builtin_bit_cast(h2, __builtin_amdgcn_cvt_pkrtz(lo, hi));
   }
   coarse = a.v, fine = b.v;
@@ -628,7 +628,7 @@ template <int D>
 constexpr int kOutPitch = D + 4;  // of the outputs in LDS
 template <int D, int R>
 constexpr size_t kv_lds() {
-  constexpr size_t loop = sizeof(KvLds<D, R>), out = (size_t)4 * 16 * kOutPitch<D> * 4 + 4 * 16 * 8 + 64;
+  constexpr size_t loop = sizeof(KvLds<D, R>), out = (size_t)4 * 16 * kOutPitch<D> * 4 + 4 * 16 * 12;
   return loop > out ? loop : out;
 }
 
@@ -662,7 +662,7 @@ __global__ __launch_bounds__(256, kv_waves(D, R)) void k_kv_attend(KvAttend a, K
   for (int rt = 0; rt < R; ++rt) {
 #pragma unroll
     for (int j = 0; j < DB; ++j) O[rt][j] = f4{0.0f, 0.0f, 0.0f, 0.0f};
-    sm[rt] = {kHidden, 0.0f, 0.0f};
+    sm[rt] = {kHidden, 0.0f, kFirstLimit};
   }
 
   const uint8_t* kp = a.k + kb * KB;
@@ -764,7 +764,7 @@ __global__ __launch_bounds__(256, kv_waves(D, R)) void k_kv_attend(KvAttend a, K
 #pragma unroll
           for (int j = 0; j < DB; ++j) O[rt][j] *= f;
         });
-        weigh_fine(s, P[rt], fine[rt]);
+        weigh_fine(s, sm[rt].per_weight(), P[rt], fine[rt]);
       }
 
       // O^T += V^T P^T, one element of d per lane column at a time
@@ -791,7 +791,7 @@ __global__ __launch_bounds__(256, kv_waves(D, R)) void k_kv_attend(KvAttend a, K
   // ---- the four waves meet, one row tile at a time
   asm volatile("" : "+v"(tid), "+v"(c), "+v"(kb));  // nor of this
   float* out = reinterpret_cast<float*>(lds_bytes);       // [wave][16][OP]
-  float* ml = out + 4 * 16 * OP;                          // [wave][16][2]
+  float* ml = out + 4 * 16 * OP;                          // [wave][16]: r, l, limit
   const bool direct = pt.used <= 1;
   float* ml_out = a.work + (int64_t)a.T * a.q_heads * sp.parts * D;
 #pragma unroll
@@ -804,27 +804,32 @@ __global__ __launch_bounds__(256, kv_waves(D, R)) void k_kv_attend(KvAttend a, K
 #pragma unroll
       for (int j = 0; j < DB; ++j) o[j] = O[rt][j][i];
     }
-    if (kb == 0) ml[(wave * 16 + c) * 2] = sm[rt].r, ml[(wave * 16 + c) * 2 + 1] = ls;
+    if (kb == 0) {
+      float* x = ml + (wave * 16 + c) * 3;
+      x[0] = sm[rt].r, x[1] = ls, x[2] = sm[rt].limit;
+    }
     __syncthreads();
     for (int x = tid; x < 16 * (D / 4); x += 256) {
       const int r = x / (D / 4), d = x % (D / 4) * 4, rr = row0 + 16 * rt + r;
       if (rr >= nq * G) continue;
-      float M = -INFINITY;
+      // Normalised here, also where parts are to meet: V's own range then bounds
+      // what is stored.  Codes were taken times 2^-9, weights in units of
+      // 2^-14 limit; 2^80 more keeps the factors in range until they meet.
+      const float* x4 = ml + 3 * r;
+      float M = x4[0], sum = 0.0f, f[4];
 #pragma unroll
-      for (int w = 0; w < 4; ++w) M = fmaxf(M, ml[(w * 16 + r) * 2]);
-      const float mu = M == -INFINITY ? 0.0f : M;
-      float sum = 0.0f, f[4];  // the outputs' codes were taken times 2^-9
-      f4 o = {0.0f, 0.0f, 0.0f, 0.0f};
+      for (int w = 1; w < 4; ++w) M = fmaxf(M, x4[48 * w]);
 #pragma unroll
       for (int w = 0; w < 4; ++w) {
-        const float e = __builtin_amdgcn_exp2f(ml[(w * 16 + r) * 2] - mu);
-        sum += ml[(w * 16 + r) * 2 + 1] * e;
-        f[w] = 512.0f * e;
+        f[w] = __builtin_amdgcn_exp2f(x4[48 * w] - M);
+        sum += x4[48 * w + 1] * f[w];
       }
-      const float by = direct ? (sum == 0.0f ? 0.0f : 1.0f / sum) : 1.0f;
+      const float by = sum == 0.0f ? 0.0f : 0x1p80f / sum;
+      f4 o = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
       for (int w = 0; w < 4; ++w)
-        o += *reinterpret_cast<const f4*>(out + (w * 16 + r) * OP + d) * (f[w] * by);
+        o += *reinterpret_cast<const f4*>(out + (w * 16 + r) * OP + d) *
+             ldexpf(f[w] * by, RowSoftmax::exponent(x4[48 * w + 2]) - 14 + 9 - 80);
       const int64_t t = span.first + rr / G, hq = (int64_t)h * G + rr % G;
       if (direct) {
         const int64_t at = t * a.o_ts + hq * a.o_hs + d;
@@ -841,6 +846,31 @@ __global__ __launch_bounds__(256, kv_waves(D, R)) void k_kv_attend(KvAttend a, K
         if (d == 0) ml_out[2 * x] = M, ml_out[2 * x + 1] = sum;
       }
     }
+  }
+}
+
+// Weighted means o of sums l relative to exp2(m), joined with K more.  A part
+// that met a NaN alone has no maximum, but its sum.
+template <int K, int E>
+__device__ __forceinline__ void join_parts(float& m, float& l, float (&o)[E], const float (&pm)[K], const float (&pl)[K],
+                                           const float (&po)[K][E]) {
+  float M = m, b[K];
+#pragma unroll
+  for (int k = 0; k < K; ++k) M = fmaxf(M, pm[k]);
+  const float a = l * __builtin_amdgcn_exp2f(m - M);
+  l = a;
+#pragma unroll
+  for (int k = 0; k < K; ++k) {
+    b[k] = pl[k] * __builtin_amdgcn_exp2f(pm[k] - M);
+    l += b[k];
+  }
+  m = M;
+  const float by = l == 0.0f ? 0.0f : 1.0f / l;
+#pragma unroll
+  for (int i = 0; i < E; ++i) {
+    o[i] *= a * by;
+#pragma unroll
+    for (int k = 0; k < K; ++k) o[i] += po[k][i] * (b[k] * by);
   }
 }
 
@@ -865,7 +895,7 @@ __global__ __launch_bounds__(256) void k_kv_join(KvAttend a, KvSplit sp) {
   if (pt.used <= 1) return;  // written where it was computed
   const float* w = a.work + x * sp.parts * D;
   const float* wml = a.work + (int64_t)a.T * a.q_heads * sp.parts * D + x * sp.parts * 2;
-  float m = -INFINITY, l = 0.0f, o[E] = {};
+  float m = kHidden, l = 0.0f, o[E] = {};
   // kAhead parts' loads at a time (past the last one: the first again, weightless)
   for (int p0 = first; p0 < pt.used; p0 += W * kAhead) {
     float pm[kAhead], pl[kAhead], po[kAhead][E];
@@ -873,19 +903,11 @@ __global__ __launch_bounds__(256) void k_kv_join(KvAttend a, KvSplit sp) {
     for (int k = 0; k < kAhead; ++k) {
       const bool on = p0 + W * k < pt.used;
       const int p = on ? p0 + W * k : p0;
-      pm[k] = on ? wml[2 * p] : -INFINITY, pl[k] = on ? wml[2 * p + 1] : 0.0f;
+      pm[k] = on ? wml[2 * p] : kHidden, pl[k] = on ? wml[2 * p + 1] : 0.0f;
 #pragma unroll
       for (int i = 0; i < E; ++i) po[k][i] = on ? w[(int64_t)p * D + E * lane + i] : 0.0f;
     }
-#pragma unroll
-    for (int k = 0; k < kAhead; ++k) {
-      const float mn = fmaxf(m, pm[k]), mu = mn == -INFINITY ? 0.0f : mn;
-      const float al = __builtin_amdgcn_exp2f(m - mu), be = __builtin_amdgcn_exp2f(pm[k] - mu);
-      l = l * al + pl[k] * be;  // a part that met a NaN alone has no maximum, but its sum
-#pragma unroll
-      for (int i = 0; i < E; ++i) o[i] = o[i] * al + po[k][i] * be;
-      m = mn;
-    }
+    join_parts(m, l, o, pm, pl, po);
   }
   if constexpr (W > 1) {
 #pragma unroll
@@ -893,28 +915,20 @@ __global__ __launch_bounds__(256) void k_kv_join(KvAttend a, KvSplit sp) {
     if (lane == 0) ml[wave][0] = m, ml[wave][1] = l;
     __syncthreads();
     if (wave) return;
-    float M = -INFINITY;
+    float pm[W - 1], pl[W - 1], po[W - 1][E];
 #pragma unroll
-    for (int k = 0; k < W; ++k) M = fmaxf(M, ml[k][0]);
-    const float mu = M == -INFINITY ? 0.0f : M;
-    l = 0.0f;
+    for (int k = 0; k < W - 1; ++k) {
+      pm[k] = ml[k + 1][0], pl[k] = ml[k + 1][1];
 #pragma unroll
-    for (int i = 0; i < E; ++i) o[i] = 0.0f;
-#pragma unroll
-    for (int k = 0; k < W; ++k) {
-      const float f = __builtin_amdgcn_exp2f(ml[k][0] - mu);
-      l += ml[k][1] * f;
-#pragma unroll
-      for (int i = 0; i < E; ++i) o[i] += out[k][E * lane + i] * f;
+      for (int i = 0; i < E; ++i) po[k][i] = out[k + 1][E * lane + i];
     }
-    m = M;
+    join_parts(m, l, o, pm, pl, po);
   }
-  const float by = l == 0.0f ? 0.0f : 1.0f / l;
   const int64_t at = t * a.o_ts + hq * a.o_hs + E * lane;
 #pragma unroll
   for (int i = 0; i < E; ++i) {
-    if (a.type == SONIQ_BF16) static_cast<uint16_t*>(a.out)[at + i] = bf16_bits(o[i] * by);
-    else static_cast<_Float16*>(a.out)[at + i] = (_Float16)(o[i] * by);
+    if (a.type == SONIQ_BF16) static_cast<uint16_t*>(a.out)[at + i] = bf16_bits(o[i]);
+    else static_cast<_Float16*>(a.out)[at + i] = (_Float16)o[i];
   }
   if (lane == 0 && a.lse) a.lse[x] = l == 0.0f ? -INFINITY : (m + __log2f(l)) * 0.693147181f;
 }

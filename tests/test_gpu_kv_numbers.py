@@ -38,3 +38,117 @@ def test_weights_are_two_fp16_numbers(dtype, bits):
     half, tiny = torch.finfo(q.dtype).eps / 2, torch.finfo(q.dtype).tiny
     ok = far <= bound + half * (np.maximum(np.abs(want), tiny) + bound)
     assert ok.all(), ((~ok).sum(), ok.size, (far - half * np.abs(want))[~ok].max(), bound.max())
+
+
+# ------------------------------------------------- scores and scales apart --
+LOG2E = float(np.log2(np.e))
+LN2 = float(np.float32(np.log(2.0)))                  # a scale of it makes scores count in powers of two
+
+
+def _told(r, scores, values, D, bits, page=16):
+    """A cache of one sequence whose position j scores scores[j] (float32)
+    against a query of 1 in element 0 and holds V codes times values[j]."""
+    n, top = len(scores), 127 if bits == 8 else 7
+    pages, table = _tables(r, [n], page)
+    cache, h = _random_cache(r, pages, page, 1, D, bits)
+    at = [(int(table[0, j // page]), 0, j % page) for j in range(n)]
+    for j, (x, v) in enumerate(zip(np.asarray(scores, np.float32), np.asarray(values, np.float32))):
+        code = np.zeros(D, np.int64)
+        code[0] = np.sign(x)
+        h["k"][at[j]], h["ks"][at[j]] = serve.pack_codes(code, bits), np.abs(x)
+        h["vs"][at[j]] = v / np.float32(top)
+    for t, x in ((cache.k, "k"), (cache.k_scale, "ks"), (cache.v_scale, "vs")):
+        t.copy_(torch.from_numpy(h[x].view(np.int8) if x == "k" else h[x]))
+    V = np.stack([serve.unpack_codes(h["v"][a], bits) * h["vs"][a].astype(np.float64) for a in at])
+    return cache, table, V
+
+
+def _check_told(scores, values, dtype, bits, D=64, seed=0):
+    """Query heads of 1, 1/2 and -1 in element 0, against float64.  Off by,
+    relatively, in each weight: two fp16 numbers 2^-21; the base-2 exponent x
+    of a weight that counts is rounded three times (the row's unit, the
+    difference from the reference, a moved reference), 2^-23 |x| each as
+    exp2 grows by ln 2 < 1; exp2 and its products 8 * 2^-24.  The sums of n
+    terms add n * 2^-24.  An exponential below 2^-126 of the row's largest may be
+    0, and a weight is off by 2^-30 of the largest one where it is subnormal."""
+    r = np.random.default_rng(seed)
+    cache, table, V = _told(r, scores, values, D, bits)
+    n = len(scores)
+    heads = np.array([1.0, 0.5, -1.0])
+    q = torch.zeros((1, 3, D), dtype=TYPES[dtype], device="cuda")
+    q[0, :, 0] = torch.from_numpy(heads).to(q.dtype)
+    lse = torch.zeros((1, 3), device="cuda")
+    out = sq.soniq_kv_attention(cache, q, torch.from_numpy(table).cuda(), _i32([0, 1]), _i32([n]), scale=LN2, lse=lse)
+    got, got_lse = out.double().cpu().numpy()[0], lse.double().cpu().numpy()[0]
+    half, tiny = torch.finfo(q.dtype).eps / 2, torch.finfo(q.dtype).tiny
+    s = np.asarray(scores, np.float32).astype(np.float64)
+    for g, a in enumerate(heads):
+        z = a * s * (LN2 * LOG2E)
+        x = z - z.max()
+        p = np.exp2(x)
+        share = p[:, None] * np.abs(V) / p.sum()
+        off = 2.0**-21 + 3 * 2.0**-23 * np.abs(x) + (8 + n) * 2.0**-24
+        total = (off * p).sum() / p.sum()             # of the sum below
+        want = p @ V / p.sum()
+        bound = (share * (off + total)[:, None]).sum(0) + n * (2.0**-126 * np.abs(V).max(0) + 2.0**-30 * share.max())
+        limit = bound + half * (np.maximum(np.abs(want), tiny) + bound)
+        far = np.abs(got[g] - want)
+        assert np.isfinite(got[g]).all(), (g, got[g][:4], want[:4])
+        assert (far <= limit).all(), (g, far.max(), limit.min(), got[g][:4], want[:4])
+        l = z.max() / LOG2E + np.log(p.sum())
+        assert abs(got_lse[g] - l) <= 1e-5 + 2.0**-21 * abs(l), (g, got_lse[g], l)
+
+
+def _spread(steps, span):
+    """Each step's (score, value) for `span` positions."""
+    return [x for x, _ in steps for _ in range(span)], [v for _, v in steps for _ in range(span)]
+
+
+APART = {  # (score in base 2, V's largest element) in the order of the positions
+    "zero V, a jump, then V far below": [(0, 0), (75, 0), (-60, 1)],
+    "zero V alone": [(0, 0), (75, 0), (-3, 0)],
+    "equal scores past 2^24": [(3e7 + 2, 0.01), (3e7 + 2, 10), (3e7 + 2, 3e4)],
+    "equal scores past 2^29": [(1e9, 0.01), (1e9, 10)],
+    "a rise that V makes up for": [(0, 1), (100, 2.0**-100)],
+    "a fall that V makes up for": [(100, 2.0**-50), (0, 2.0**50)],
+    "V all tiny": [(0, 2.0**-100), (1, 2.0**-101), (-4, 2.0**-99)],
+    "V all huge": [(0, 2.0**120), (3, 2.0**117), (1, 2.0**119)],
+    "steps up": [(30 * i, 2.0**(-30 * i)) for i in range(4)],
+    "steps down": [(-30 * i, 2.0**(30 * i)) for i in range(4)],
+    "up and down": [(0, 1), (90, 2.0**-90), (10, 2.0**-12), (89, 2.0**-91), (-5, 32)],
+}
+
+
+@pytest.mark.parametrize("bits", [8, 4])
+@pytest.mark.parametrize("span", [32, 128, 700])      # by waves, by steps of a wave, by parts
+@pytest.mark.parametrize("name", list(APART))
+def test_scores_and_scales_far_apart(name, span, bits):
+    _check_told(*_spread(APART[name], span), "bf16", bits)
+
+
+@pytest.mark.parametrize("span", [32, 128, 700])
+def test_scores_far_apart_fp16(span):
+    for steps in ([(1e9, 0.01), (1e9, 10)], [(0, 1), (12, 2.0**-12)], [(0, 0), (75, 0), (74, 3)]):
+        _check_told(*_spread(steps, span), "fp16", 8)
+
+
+def test_a_wave_far_below_the_others():
+    """One wave meets zero V and a jump, the others scores so far above that
+    nothing of that wave counts."""
+    scores, values = [], []
+    for step in ((0, 0), (75, 0), (-60, 1)):
+        for wave in range(4):
+            scores += [step[0] if wave == 0 else 215 + wave] * 32
+            values += [step[1] if wave == 0 else 0.5] * 32
+    _check_told(scores, values, "bf16", 8)
+
+
+def test_rows_of_zeros_beside_others():
+    """V rows of zeros as soniq_kv_write leaves them (scale 0), keys with
+    scores on both sides of the others'."""
+    r = np.random.default_rng(33)
+    for spread in (1.0, 12.0, 60.0):
+        scores = spread * r.standard_normal(900)
+        values = np.where(r.random(900) < 0.6, 0.0, np.exp2(r.integers(-8, 9, 900)))
+        values[:300] = 0
+        _check_told(scores, values, "bf16", 8)
