@@ -179,11 +179,11 @@ __global__ __launch_bounds__(256) void k_kv_copy(KvCopy c, int tw) {
 // Softmax of a row over the positions so far, all in fp32 and base 2:
 //   p = exp2(s - r),  l = sum p,  w = p * s_v,  outputs = sum w * code.
 // The reference r has to do with scores alone: one that was met, so that l
-// neither overflows nor vanishes.  It moves only where a p passes 2^80.  The
-// weights go into the product as fp16, in a unit of their own, a power of two
-// that follows the largest w so far (between 2^6 and 2^14 units of it): only
-// exponents change with it, so that scores and V scales may rise and fall
-// against each other over all of fp32's range.  Both are rarely moved.
+// neither overflows nor vanishes.  The weights go into the product as fp16, in
+// a unit of their own, a power of two that follows the largest w so far
+// (between 2^6 and 2^14 units of it): only exponents change with it, so that
+// scores and V scales may rise and fall against each other over all of fp32's
+// range.  Both are rarely moved: where a p passes 2^80, or a w its 2^14 units.
 // Half a step of fp16 in each weight is as much as an fp16 output's own and an
 // eighth of a bf16 output's, so a second product takes what the rounding left
 // (without it, fp16 outputs' error against 64 bits was 1.4 to 1.5 times that of
@@ -243,24 +243,28 @@ __device__ __forceinline__ void softmax_step(float (&x)[N], const float (&v)[N],
     }
   };
   weigh();
-  if (__any(lt > 0x1p80f || top > st.limit)) {
+  const uint64_t hot = __ballot(lt > 0x1p80f || top > st.limit);
+  if (hot) {
+    uint32_t rows = (uint32_t)(hot | hot >> 32);  // bit c: row c, by any of its four lanes
+    rows |= rows >> 16;
+    const bool moves = rows >> (threadIdx.x % 16) & 1;
     float mx = x[0];
 #pragma unroll
     for (int e = 1; e < N; ++e) mx = fmaxf(mx, x[e]);
     mx = quad_max(mx * qf);
+    // A row's reference moves up to the highest score with its weights' unit:
+    // with exponentials up to 1 no weight can pass fp32's end before it is
+    // scaled, and the sum has room.
     float f = 1.0f;
-    if (mx > st.r + 80.0f) {  // the first positions, or scores far above those before
+    if (moves && mx > st.r) {
       f = __builtin_amdgcn_exp2f(st.r - mx);
       st.r = mx;
     }
     weigh();
-    const int was = RowSoftmax::exponent(st.limit) - 8;  // of the largest weight when the unit was chosen
-    int e = was;
     top = quad_max(top);
-    if (f != 1.0f || top > st.limit) {
-      e = min(max(RowSoftmax::exponent(fmaxf(ldexpf(f, was), top)), -120), 119);
-      st.limit = RowSoftmax::power(e + 8);
-    }
+    const int was = RowSoftmax::exponent(st.limit) - 8;  // of the largest weight when the unit was chosen
+    const int e = moves ? min(max(RowSoftmax::exponent(fmaxf(ldexpf(f, was), top)), -120), 119) : was;
+    st.limit = RowSoftmax::power(e + 8);
     st.l *= f;
     scale(ldexpf(f, was - e));
   }

@@ -152,3 +152,12 @@ def test_rows_of_zeros_beside_others():
         values = np.where(r.random(900) < 0.6, 0.0, np.exp2(r.integers(-8, 9, 900)))
         values[:300] = 0
         _check_told(scores, values, "bf16", 8)
+
+
+@pytest.mark.parametrize("bits", [8, 4])
+@pytest.mark.parametrize("span", [32, 128, 700])
+@pytest.mark.parametrize("rise", [20, 39, 60, 79])
+def test_a_rise_onto_large_values(rise, span, bits):
+    """Scores that rise by less than any step of a reference, onto V whose
+    product with an unnormalised exponential would pass fp32's end."""
+    _check_told(*_spread([(0, 1), (rise, 2.0**110), (rise - 3, 2.0**113)], span), "bf16", bits)
