@@ -639,7 +639,9 @@ soniq_status soniq_kv_read(const soniq_kv_cache_t* cache, void* K_dev, int64_t k
  *     without a mask: positions up to its own, base + i;
  *     with a mask: position base + j where bit j % 64 of word j / 64 of row
  *     cu[b] + i is set (a tree of drafted tokens: its ancestors and itself).
- * A query that sees nothing gets zeros (and lse -inf).
+ * A query that sees nothing gets zeros (and lse -inf).  One that sees a key
+ * whose scale is infinite or NaN, as soniq_kv_write stores a row that held an
+ * infinity or a NaN, gets NaN; positions that it does not see may hold anything.
  *   q_dev      device, type SONIQ_BF16 or SONIQ_F16 [T, q_heads, head_dim];
  *              strides in elements, head_dim contiguous; q_heads a multiple
  *              of the cache's heads: query head h reads head

@@ -614,10 +614,16 @@ struct KvFind {
       }
     }
   }
+  // A key whose scale is infinite holds no numbers (soniq_kv_write stores a row
+  // with an infinity as codes 0): its score is NaN, never an infinity of the
+  // sign of whatever the codes sum up to, since -inf would hide the position.
   __device__ __forceinline__ void scales(int n, int tid, KvPositions& L) const {
 #pragma unroll
     for (int k = 0; k < kSub / 256; ++k)
-      if (256 * k < n) L.ks[tid + 256 * k] = ks[k], L.vs[tid + 256 * k] = vs[k];
+      if (256 * k < n) {
+        L.ks[tid + 256 * k] = __builtin_isinf(ks[k]) ? __builtin_nanf("") : ks[k];
+        L.vs[tid + 256 * k] = vs[k];
+      }
   }
 };
 

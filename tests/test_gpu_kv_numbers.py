@@ -161,3 +161,46 @@ def test_a_rise_onto_large_values(rise, span, bits):
     """Scores that rise by less than any step of a reference, onto V whose
     product with an unnormalised exponential would pass fp32's end."""
     _check_told(*_spread([(0, 1), (rise, 2.0**110), (rise - 3, 2.0**113)], span), "bf16", bits)
+
+
+# ------------------------------------------------------- rows with no value --
+@pytest.mark.parametrize("bits", [8, 4])
+@pytest.mark.parametrize("dtype", ["bf16", "fp16"])
+@pytest.mark.parametrize("side", ["k", "v"])
+def test_a_visible_row_that_held_an_infinity(side, dtype, bits):
+    """A key or value row with an infinity is stored as scale inf and codes 0,
+    so its elements are NaN: every query that sees it gets NaN, whatever its
+    own values, and no other query does."""
+    r = np.random.default_rng(34)
+    held, new, heads, group, D = 90, 40, 2, 4, 128
+    pages, table = _tables(r, [held + new], 16)
+    cache, h = _random_cache(r, pages, 16, heads, D, bits)
+    kv = torch.from_numpy(r.standard_normal((2, new, heads, D)).astype(np.float32)).cuda()
+    where = 13                                         # this new token's row, in head 1
+    kv["kv".index(side), where, 1, 7] = float("inf") if bits == 8 else -float("inf")
+    args = (torch.from_numpy(table).cuda(), _i32([0, new]))
+    sq.soniq_kv_write(cache, kv[0], kv[1], *args, _i32([held]))
+    q = r.standard_normal((new, heads * group, D)).astype(np.float32)
+    q[1::4, :, 5] *= 300                               # an outlier channel
+    q[2::4] *= np.exp2(r.integers(-12, 5, D))          # a wide range
+    q[3::4] *= 0.01
+    q = torch.from_numpy(q).to(TYPES[dtype]).cuda()
+    out = sq.soniq_kv_attention(cache, q, *args, _i32([held + new]))
+    bad = torch.zeros((new, heads * group), dtype=torch.bool)
+    bad[where:, group:] = True                         # causal: that token and those after it
+    nan = torch.isnan(out).cpu()
+    assert bool(nan[bad].all()), int((~nan[bad].all(-1)).sum())
+    assert not bool(nan[~bad].any())
+
+
+@pytest.mark.parametrize("sign", [1, -1])
+def test_an_infinite_scale_over_codes(sign):
+    """A caller's own cache may hold an infinite K scale over any codes: NaN
+    as well, not a score of minus infinity that drops the position."""
+    r = np.random.default_rng(35)
+    pages, table = _tables(r, [70], 16)
+    cache, h = _random_cache(r, pages, 16, 1, 64, 8)
+    cache.k_scale[int(table[0, 1]), 0, 3] = sign * float("inf")
+    q = torch.from_numpy(r.standard_normal((2, 8, 64)).astype(np.float32)).to(torch.bfloat16).cuda()
+    out = sq.soniq_kv_attention(cache, q, torch.from_numpy(table).cuda(), _i32([0, 2]), _i32([70]))
+    assert bool(torch.isnan(out).all())
