@@ -168,13 +168,13 @@ __global__ __launch_bounds__(256) void k_kv_copy(KvCopy c, int tw) {
 // each position's cache row and scales.
 //
 // Codes become fp16 exactly: a code moved to unsigned, u = code + zero, is the
-// fp16 subnormal u * 2^-24.  K goes into the product like that, and the
-// scores start from -zero * 2^-24 * sum(q) (sums of D terms: nothing is
-// lost); V would lose digits over a long context, so one packed fma makes it
-// (u - zero) * 2^-9 first.
+// fp16 subnormal u * 2^-24, and one packed fma a pair makes it (u - zero) * 2^-15
+// for K and 2^-9 for V.  (K could do without, with scores that start from
+// -zero * sum(q): 3 to 4% less with many rows, but their sums then round at the
+// size of u, which moved scores of 4-bit keys by 20 times what an fp32 sum is
+// off by, and by 2e-4 where one channel was 30 times the others.)
 // Queries are scaled by a power of two per row to use fp16's whole range
-// (bf16 queries are exact in it down to 2^-22 of the row's largest element,
-// the sixteenths that meet odd 4-bit codes too).
+// (bf16 queries are exact in it down to 2^-22 of the row's largest element).
 //
 // Softmax of a row over the positions so far, all in fp32 and base 2:
 //   p = exp2(s - r),  l = sum p,  w = p * s_v,  outputs = sum w * code.
@@ -290,34 +290,31 @@ __device__ __forceinline__ void weigh_fine(const float (&w)[8], float units, h8&
   coarse = a.v, fine = b.v;
 }
 
-// Two V codes moved to unsigned, times 2^-9.
-// (UP: times 16 before that, as they lie in the odd nibbles.)
-template <int BITS, bool UP>
-__device__ __forceinline__ h2 v_half(uint32_t u16pair) {
-  const h2 x = __builtin_bit_cast(h2, u16pair);
-  const _Float16 z = BITS == 8 ? (_Float16)-0.25f : (_Float16)-0x1p-6f, m = UP ? (_Float16)2048.0f : (_Float16)32768.0f;
-  return __builtin_elementwise_fma(x, h2{m, m}, h2{z, z});
+// Two codes moved to unsigned and held as fp16 subnormals (UP: times 16, as they
+// lie in the odd nibbles): the codes times 2^UNIT, exactly.
+template <int BITS, bool UP, int UNIT>
+__device__ __forceinline__ h2 signed_half(uint32_t u16pair) {
+  constexpr float up = (float)(1 << (24 + UNIT)) / (UP ? 16 : 1), zero = (BITS == 8 ? 128.0f : 8.0f) / (float)(1 << -UNIT);
+  constexpr _Float16 m = (_Float16)up, z = (_Float16)-zero;
+  return __builtin_elementwise_fma(__builtin_bit_cast(h2, u16pair), h2{m, m}, h2{z, z});
 }
+constexpr int kUnitK = -15, kUnitV = -9;
 
 // Eight K codes as an operand: from two words of 8-bit codes in order, or
-// from one word of 4-bit codes in the order 0 4 1 5 2 6 3 7, the odd ones
-// times 16 (no shift; the queries hold a sixteenth there).
+// from one word of 4-bit codes in the order 0 4 1 5 2 6 3 7.
 template <int BITS>
 __device__ __forceinline__ h8 k_operand(const uint32_t* w) {
-  union { uint32_t p[4]; h8 v; } r;
-  if constexpr (BITS == 8) {
+  union { h2 p[4]; h8 v; } r;
 #pragma unroll
-    for (int i = 0; i < 2; ++i) {
+  for (int i = 0; i < 2; ++i) {
+    if constexpr (BITS == 8) {
       const uint32_t u = w[i] ^ 0x80808080u;
-      r.p[2 * i] = __builtin_amdgcn_perm(u, u, 0x0c010c00u);
-      r.p[2 * i + 1] = __builtin_amdgcn_perm(u, u, 0x0c030c02u);
-    }
-  } else {
-#pragma unroll
-    for (int i = 0; i < 2; ++i) {
+      r.p[2 * i] = signed_half<8, false, kUnitK>(__builtin_amdgcn_perm(u, u, 0x0c010c00u));
+      r.p[2 * i + 1] = signed_half<8, false, kUnitK>(__builtin_amdgcn_perm(u, u, 0x0c030c02u));
+    } else {
       const uint32_t u = w[0] >> (8 * i);
-      r.p[2 * i] = (u ^ 0x00080008u) & 0x000F000Fu;
-      r.p[2 * i + 1] = (u ^ 0x00800080u) & 0x00F000F0u;
+      r.p[2 * i] = signed_half<4, false, kUnitK>((u ^ 0x00080008u) & 0x000F000Fu);
+      r.p[2 * i + 1] = signed_half<4, true, kUnitK>((u ^ 0x00800080u) & 0x00F000F0u);
     }
   }
   return r.v;
@@ -379,7 +376,7 @@ __device__ __forceinline__ h8 v_operand(const Raw<VB> (&r)[8], int j) {
       hi = ODD ? (hi ^ 0x80808080u) & 0xF0F0F0F0u : (hi ^ 0x08080808u) & 0x0F0F0F0Fu;
     }
     const uint32_t by = j * BITS / 8 % 4;
-    x.p[i] = v_half<BITS, BITS == 4 && ODD>(__builtin_amdgcn_perm(hi, lo, 0x0c000c00u | (4 + by) << 16 | by));
+    x.p[i] = signed_half<BITS, BITS == 4 && ODD, kUnitV>(__builtin_amdgcn_perm(hi, lo, 0x0c000c00u | (4 + by) << 16 | by));
   }
   return x.v;
 }
@@ -509,10 +506,10 @@ __device__ __forceinline__ bool kv_unit(const KvAttend& a, const KvSplit& sp, in
   return u.rows > 0 && (u.part == 0 || u.pt.count > 0);
 }
 
-// Per query row: the unit of its scores, where they start, its query (-1: none).
+// Per query row: the unit of its scores, its query (-1: none).
 template <int ROWS>
 struct KvRowInfo {
-  float qf[ROWS], qz[ROWS];
+  float qf[ROWS];
   int32_t qi[ROWS];
 };
 
@@ -556,27 +553,17 @@ struct KvQuery {
     int e = (int)(mx >> 23) - 127 - 14;
     e = mx >= 0x7F800000u || mx == 0 ? 0 : max(e, -100);
     const float down = copysignf(__uint_as_float((uint32_t)(127 - e) << 23), a.scale);
-    float sum = 0.0f;
 #pragma unroll
     for (int g = 0; g < PER / 8; ++g) {
       h8 v;
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        constexpr float kOdd = BITS == 4 ? 16.0f : 1.0f;  // as k_operand takes them
-        const float unit = i % 2 ? kOdd : 1.0f;
-        const _Float16 y = (_Float16)(value(8 * g + i) * (down * (1.0f / unit)));
-        v[k_order<BITS>(i)] = y;
-        sum += (float)y * unit;
-      }
+      for (int i = 0; i < 8; ++i) v[k_order<BITS>(i)] = (_Float16)(value(8 * g + i) * down);
       const int d = d0 + 8 * g;
       q[r / 16][d % (D / 4) / 8][d / (D / 4) * 16 + r % 16] = v;
     }
-#pragma unroll
-    for (int o = 1; o < TPR; o *= 2) sum += __shfl_xor(sum, o);
     if (tid % TPR == 0) {
       // (never 0: hidden positions stay at -inf)
-      info.qf[r] = fmaxf(fabsf(a.scale) * 1.44269504f * 0x1p24f * __uint_as_float((uint32_t)(127 + e) << 23), 0x1p-126f);
-      info.qz[r] = sum * (BITS == 8 ? -0x1p-17f : -0x1p-21f);
+      info.qf[r] = fmaxf(fabsf(a.scale) * 1.44269504f * (float)(1 << -kUnitK) * __uint_as_float((uint32_t)(127 + e) << 23), 0x1p-126f);
       info.qi[r] = r < u.rows ? (u.row0 + r) / a.group : -1;
     }
   }
@@ -722,12 +709,7 @@ __global__ __launch_bounds__(256, kv_waves(D, R)) void k_kv_attend(KvAttend a, K
       const bool more = st + 4 < nst;
       f4 S[R][2];
 #pragma unroll
-      for (int rt = 0; rt < R; ++rt) {
-        int x = 16 * rt + c;
-        asm volatile("" : "+v"(x));
-        const float z = L.info.qz[x];
-        S[rt][0] = S[rt][1] = f4{z, z, z, z};
-      }
+      for (int rt = 0; rt < R; ++rt) S[rt][0] = S[rt][1] = f4{0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
       for (int s = 0; s < NK; ++s) {
         if constexpr (D * R > 256) __builtin_amdgcn_sched_barrier(0);
@@ -823,8 +805,8 @@ __global__ __launch_bounds__(256, kv_waves(D, R)) void k_kv_attend(KvAttend a, K
       const int r = x / (D / 4), d = x % (D / 4) * 4, rr = row0 + 16 * rt + r;
       if (rr >= nq * G) continue;
       // Normalised here, also where parts are to meet: V's own range then bounds
-      // what is stored.  Codes were taken times 2^-9, weights in units of
-      // 2^-14 limit; 2^80 more keeps the factors in range until they meet.
+      // what is stored.  Codes were taken times 2^kUnitV, weights in units
+      // of 2^-14 limit; 2^80 more keeps the factors in range until they meet.
       const float* x4 = ml + 3 * r;
       float M = x4[0], sum = 0.0f, f[4];
 #pragma unroll
@@ -839,7 +821,7 @@ __global__ __launch_bounds__(256, kv_waves(D, R)) void k_kv_attend(KvAttend a, K
 #pragma unroll
       for (int w = 0; w < 4; ++w)
         o += *reinterpret_cast<const f4*>(out + (w * 16 + r) * OP + d) *
-             ldexpf(f[w] * by, RowSoftmax::exponent(x4[48 * w + 2]) - 14 + 9 - 80);
+             ldexpf(f[w] * by, RowSoftmax::exponent(x4[48 * w + 2]) - 14 - kUnitV - 80);
       const int64_t t = span.first + rr / G, hq = (int64_t)h * G + rr % G;
       if (direct) {
         const int64_t at = t * a.o_ts + hq * a.o_hs + d;

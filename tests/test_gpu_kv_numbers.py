@@ -204,3 +204,62 @@ def test_an_infinite_scale_over_codes(sign):
     q = torch.from_numpy(r.standard_normal((2, 8, 64)).astype(np.float32)).to(torch.bfloat16).cuda()
     out = sq.soniq_kv_attention(cache, q, torch.from_numpy(table).cuda(), _i32([0, 2]), _i32([70]))
     assert bool(torch.isnan(out).all())
+
+
+@pytest.mark.parametrize("bits", [8, 4])
+@pytest.mark.parametrize("dtype", ["bf16", "fp16"])
+def test_codes_of_zero_add_nothing(dtype, bits):
+    """Keys with one outlier channel have codes 0 elsewhere.  Queries that are
+    0 in that channel score exactly 0, whatever the scale: the mean of V."""
+    r = np.random.default_rng(36)
+    n, D = 200, 128
+    pages, table = _tables(r, [n], 16)
+    cache, h = _random_cache(r, pages, 16, 1, D, bits)
+    h["k"][:] = serve.pack_codes(np.where(np.arange(D) == 4, 127 if bits == 8 else 7, 0), bits)
+    h["ks"][:] = np.exp2(r.integers(0, 24, h["ks"].shape))
+    cache.k.copy_(torch.from_numpy(h["k"].view(np.int8)))
+    cache.k_scale.copy_(torch.from_numpy(h["ks"]))
+    q = r.standard_normal((5, 8, D)).astype(np.float32)
+    q[2] *= np.exp2(r.integers(-9, 6, D))
+    q[:, :, 4] = 0
+    q = torch.from_numpy(q).to(TYPES[dtype]).cuda()
+    lse = torch.zeros((5, 8), device="cuda")
+    out = sq.soniq_kv_attention(cache, q, torch.from_numpy(table).cuda(), _i32([0, 5]), _i32([n]), lse=lse)
+    V = np.concatenate([serve.unpack_codes(h["v"][p, 0], bits) * h["vs"][p, 0, :, None].astype(np.float64)
+                        for p in table[0]])
+    half = torch.finfo(q.dtype).eps / 2
+    for i in range(5):
+        m = n - 4 + i
+        want, size = V[:m].mean(0), np.abs(V[:m]).mean(0)
+        # a weight 2^-21 and the sums' m roundings, in the numerator and below
+        bound = size * (2.0**-21 + 2 * m * 2.0**-24)
+        assert (np.abs(out[i].double().cpu().numpy() - want) <= bound + half * (np.abs(want) + bound)).all()
+        assert np.abs(lse[i].cpu().numpy() - np.log(m)).max() <= 1e-5
+
+
+@pytest.mark.parametrize("bits", [8, 4])
+@pytest.mark.parametrize("dtype", ["bf16", "fp16"])
+@pytest.mark.parametrize("outlier", [1, 30, 1000])
+def test_a_score_is_an_fp32_sum(outlier, dtype, bits):
+    """One position a sequence, so that lse is the score itself, of keys with
+    one channel above the others and queries that are 0 there: off by D + 8
+    roundings of 2^-24 of the products' sizes (the sum's, the scalings' and
+    lse's), and of those alone."""
+    r = np.random.default_rng(37)
+    B, D = 300, 128
+    K = r.standard_normal((B, 2, D)).astype(np.float32)
+    K[:, :, 5] *= outlier
+    cache = sq.KVCache.empty(B, 16, 2, D, bits)
+    table, cu, one = _i32(np.arange(B)[:, None].tolist()), _i32(list(range(B + 1))), _i32([1] * B)
+    k = torch.from_numpy(K).cuda()
+    sq.soniq_kv_write(cache, k, k, table, cu, _i32([0] * B))
+    q = r.standard_normal((B, 8, D)).astype(np.float32)
+    q[1::2, :, 5] = 0
+    q = torch.from_numpy(q).to(TYPES[dtype]).cuda()
+    lse = torch.zeros((B, 8), device="cuda")
+    sq.soniq_kv_attention(cache, q, table, cu, one, lse=lse, max_q=1, max_kv=1)
+    codes, scales = serve.quantize_rows(K, 127.0 if bits == 8 else 7.0)
+    key = np.repeat(codes * scales[..., None].astype(np.float64), 4, axis=1)
+    products = q.double().cpu().numpy() * key * D**-0.5
+    far = np.abs(lse.double().cpu().numpy() - products.sum(-1))
+    assert (far <= (D + 8) * 2.0**-24 * np.abs(products).sum(-1)).all(), far.max()
