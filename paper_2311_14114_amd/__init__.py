@@ -863,7 +863,10 @@ def soniq_kv_attention(cache: KVCache, q, page_table, cu, kv_len, scale=None, ma
         _is(mask, "mask", d, torch.int64, 2)
         if mask.shape[0] != T or not mask.is_contiguous():
             raise ValueError("mask must be a contiguous [T, words] tensor")
-        words, bits = mask.shape[1], mask.data_ptr()
+        if mask.shape[1] == 0:                        # its address is null: the library would see no mask
+            raise ValueError("mask must have at least one word")
+        if T:
+            words, bits = mask.shape[1], mask.data_ptr()
     if lse is not None:
         _is(lse, "lse", d, torch.float32, 2)
         if lse.shape[0] != T or lse.shape[1] != heads or not lse.is_contiguous():

@@ -499,6 +499,20 @@ def test_binding_refusals():
             call()
 
 
+def test_masks_without_a_word_or_a_token():
+    """An empty mask has a null address, which is no mask: without words it is
+    refused, since it would hide every new token; without tokens there is
+    nothing to hide."""
+    cache = sq.KVCache.empty(4, 16, 2, 64)
+    t, ln = _i32([[0, 1]]), _i32([20])
+    for T in (3, 0):
+        q = torch.zeros((T, 4, 64), dtype=torch.bfloat16, device="cuda")
+        mask = torch.zeros((T, 1), dtype=torch.int64, device="cuda")
+        assert sq.soniq_kv_attention(cache, q, t, _i32([0, T]), ln, mask=mask).shape == (T, 4, 64)
+        with pytest.raises(ValueError):
+            sq.soniq_kv_attention(cache, q, t, _i32([0, T]), ln, mask=mask[:, :0].contiguous())
+
+
 def test_no_sequences_and_no_tokens():
     cache = sq.KVCache.empty(4, 16, 2, 64)
     none = torch.empty((0, 2), dtype=torch.int32, device="cuda")
