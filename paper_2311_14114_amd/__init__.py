@@ -842,8 +842,9 @@ def soniq_kv_attention(cache: KVCache, q, page_table, cu, kv_len, scale=None, ma
     mask (int64 [T, words]): bit j % 64 of word j / 64 of a row says whether
     that token sees new token j of its sequence; None: each sees the new ones
     up to itself.  scale: 1 / sqrt(head_dim) unless given.  max_q: the most
-    new tokens of a sequence (T unless given; at most 256); max_kv: the
-    longest kv_len, a hint.  lse: a float32 [T, q_heads] tensor to fill.
+    new tokens of a sequence, at most 256 (T unless given; has to be given for
+    batches of more than 256 tokens, however few of each sequence); max_kv:
+    the longest kv_len, a hint.  lse: a float32 [T, q_heads] tensor to fill.
     work: a uint8 device tensor of soniq_kv_attention_workspace(...) bytes
     (allocated when None).  Returns out (like q)."""
     d, B, width, ld, table, cu, kv_len = _kv_batch(cache, page_table, cu, kv_len, "kv_len")
@@ -872,6 +873,8 @@ def soniq_kv_attention(cache: KVCache, q, page_table, cu, kv_len, scale=None, ma
         if lse.shape[0] != T or lse.shape[1] != heads or not lse.is_contiguous():
             raise ValueError("lse must be a contiguous [T, q_heads] tensor")
     if max_q is None:
+        if T > 256:                                   # the sequences' numbers are on the device
+            raise ValueError(f"q has {T} tokens: give max_q, the most of one sequence (at most 256)")
         max_q = max(T, 1)
     if max_kv is None:
         max_kv = width * cache.page_size

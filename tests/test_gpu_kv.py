@@ -513,6 +513,20 @@ def test_masks_without_a_word_or_a_token():
             sq.soniq_kv_attention(cache, q, t, _i32([0, T]), ln, mask=mask[:, :0].contiguous())
 
 
+def test_more_tokens_than_a_sequence_may_have():
+    """300 sequences of one new token each: max_q has to be given, and the
+    refusal says so."""
+    r = np.random.default_rng(26)
+    lens = r.integers(1, 40, 300).tolist()
+    pages, table = _tables(r, lens, 16)
+    cache, h = _random_cache(r, pages, 16, 1, 64, 8)
+    q = torch.from_numpy(r.standard_normal((300, 2, 64)).astype(np.float32)).to(torch.bfloat16).cuda()
+    cu = list(range(301))
+    with pytest.raises(ValueError, match="max_q"):
+        sq.soniq_kv_attention(cache, q, torch.from_numpy(table).cuda(), _i32(cu), _i32(lens))
+    _check_attention(cache, h, q, table, cu, lens, 8, max_q=1)
+
+
 def test_no_sequences_and_no_tokens():
     cache = sq.KVCache.empty(4, 16, 2, 64)
     none = torch.empty((0, 2), dtype=torch.int32, device="cuda")
