@@ -61,8 +61,8 @@ __device__ __forceinline__ void lds_barrier() {
 // ------------------------------------------------------------ quantizing --
 __device__ __forceinline__ void store_codes(int8_t* q, int k, int K, uint2 c) {
   if (k + 8 <= K) {
-    struct __attribute__((packed, aligned(1))) P { uint2 v; };
-    reinterpret_cast<P*>(q + k)->v = c;
+    struct __attribute__((packed, aligned(1))) P { uint32_t x, y; };
+    *reinterpret_cast<P*>(q + k) = {c.x, c.y};
   } else {
     for (int i = 0; i < 8; ++i)
       if (k + i < K) q[k + i] = (int8_t)((i < 4 ? c.x : c.y) >> (8 * (i % 4)));
