@@ -649,7 +649,8 @@ soniq_status soniq_kv_read(const soniq_kv_cache_t* cache, void* K_dev, int64_t k
  *   kv_len_dev device, int32 [B]
  *   mask_dev   device, uint64 [T, mask_words], or NULL (mask_words then 0);
  *              tokens past the mask's 64 * mask_words bits are not seen
- *   scale      finite, of either sign
+ *   scale      finite, of either sign; scores (scale * q . k) have to lie in
+ *              fp32's range
  *   max_q      the largest n, at most 256; queries of a sequence from max_q
  *              on are not computed (their rows are left as they were)
  *   max_kv     the largest kv_len; only a hint for the split of the work,
@@ -661,6 +662,10 @@ soniq_status soniq_kv_read(const soniq_kv_cache_t* cache, void* K_dev, int64_t k
  *              soniq_kv_attention_workspace gives for the same T, q_heads,
  *              B, max_q, max_kv; holds nothing between calls, and calls
  *              that may overlap need one each
+ * Scores, the softmax and the sums are fp32, for any q, keys and V scales; of
+ * a row of q, elements below 2^-28 of its largest are rounded to multiples of
+ * 2^-38 of it; softmax weights are off by at most 2^-21 of themselves and
+ * 2^-30 of the largest.
  * T = 0 or B = 0 does nothing.  The same arguments give the same bits on
  * every call.  Errors: INVALID_ARGUMENT, UNSUPPORTED (T * q_heads >= 2^24,
  * B * heads * query rows / 16 >= 2^22, and the limits above), HIP.

@@ -173,8 +173,8 @@ __global__ __launch_bounds__(256) void k_kv_copy(KvCopy c, int tw) {
 // -zero * sum(q): 3 to 4% less with many rows, but their sums then round at the
 // size of u, which moved scores of 4-bit keys by 20 times what an fp32 sum is
 // off by, and by 2e-4 where one channel was 30 times the others.)
-// Queries are scaled by a power of two per row to use fp16's whole range
-// (bf16 queries are exact in it down to 2^-22 of the row's largest element).
+// Queries are scaled by a power of two per row to use fp16's whole range (they
+// are exact in it down to 2^-28 of the row's largest element).
 //
 // Softmax of a row over the positions so far, all in fp32 and base 2:
 //   p = exp2(s - r),  l = sum p,  w = p * s_v,  outputs = sum w * code.
@@ -551,7 +551,7 @@ struct KvQuery {
     for (int o = 1; o < TPR; o *= 2) mx = max(mx, (uint32_t)__shfl_xor((int)mx, o));
     // largest element to [2^14, 2^15); rows of zeros, infinities or NaN as they are
     int e = (int)(mx >> 23) - 127 - 14;
-    e = mx >= 0x7F800000u || mx == 0 ? 0 : max(e, -100);
+    e = mx >= 0x7F800000u || mx == 0 ? 0 : max(e, -126);
     const float down = copysignf(__uint_as_float((uint32_t)(127 - e) << 23), a.scale);
 #pragma unroll
     for (int g = 0; g < PER / 8; ++g) {

@@ -263,3 +263,24 @@ def test_a_score_is_an_fp32_sum(outlier, dtype, bits):
     products = q.double().cpu().numpy() * key * D**-0.5
     far = np.abs(lse.double().cpu().numpy() - products.sum(-1))
     assert (far <= (D + 8) * 2.0**-24 * np.abs(products).sum(-1)).all(), far.max()
+
+
+@pytest.mark.parametrize("bits", [8, 4])
+@pytest.mark.parametrize("power", [-114, -60, 60, 118])
+def test_queries_of_any_size(power, bits):
+    """Queries of 2^power against keys of its reciprocal: the scores of
+    ordinary ones, to the same roundings as above."""
+    r = np.random.default_rng(38)
+    B, D = 100, 128
+    K = (r.standard_normal((B, 1, D)) * 2.0**-power).astype(np.float32)
+    cache = sq.KVCache.empty(B, 16, 1, D, bits)
+    table, cu, one = _i32(np.arange(B)[:, None].tolist()), _i32(list(range(B + 1))), _i32([1] * B)
+    k = torch.from_numpy(K).cuda()
+    sq.soniq_kv_write(cache, k, k, table, cu, _i32([0] * B))
+    q = torch.from_numpy((r.standard_normal((B, 4, D)) * 2.0**power).astype(np.float32)).to(torch.bfloat16).cuda()
+    lse = torch.zeros((B, 4), device="cuda")
+    sq.soniq_kv_attention(cache, q, table, cu, one, lse=lse, max_q=1, max_kv=1)
+    codes, scales = serve.quantize_rows(K, 127.0 if bits == 8 else 7.0)
+    products = q.double().cpu().numpy() * (codes * scales[..., None].astype(np.float64)) * D**-0.5
+    far = np.abs(lse.double().cpu().numpy() - products.sum(-1))
+    assert (far <= (D + 8) * 2.0**-24 * np.abs(products).sum(-1)).all(), far.max()
