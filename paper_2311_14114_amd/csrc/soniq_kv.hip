@@ -928,23 +928,33 @@ __global__ __launch_bounds__(256) void k_kv_join(KvAttend a, KvSplit sp) {
 // Rows a workgroup takes, and how the positions are cut.  A part costs its
 // workgroup a start of several dependent loads, and 4 bytes an output written
 // and read again; and parts that are not all resident end unevenly.  So up to
-// 64 sequences are cut on the device, by their lengths (see kv_chunk).  Parts
-// have at most 1024 positions a row tile, and about eight thousand workgroups
-// a call where that gives longer ones.  Two row tiles and short parts: two
-// workgroups a CU, held there by LDS that nobody uses, finish sooner than
-// three with shorter parts yet.  Eight sequences of 3001 to 8191 positions, 8
-// heads of 128, 8 bits, us a call in a graph:
-//   rows  four workgroups a CU by the longest  by lengths, two   three
-//     20                 35.0                      28.2          28.8
-//     64                 49.2                      42            39.6
-//     96                 65.5                      66            53.5
-// (96 rows, 4 bits, fp16: 61.2, 67.7, 55.6.)
+// 64 sequences are cut on the device, by their lengths (see kv_chunk).  Times
+// below are us a call in a graph, 8 heads of 128, 8 bits, bf16.
+//  - Parts have at most 1024 positions a row tile, or more where that would
+//    make more than eight thousand workgroups (32 sequences of 2000 to 32768
+//    positions: 203, 217 with two thousand, 203 with 32 thousand; 64 of 20000
+//    to 32768: 648, 659, 658).
+//  - Two row tiles and short parts: two workgroups a CU, held there by LDS that
+//    nobody uses, finish sooner than three with shorter parts yet; three where
+//    two would have parts past nine pieces.  Cut by the longest sequence, and by
+//    lengths with two and with three:
+//      sequences  positions     rows   longest   two   three
+//          4     1001 to 4191     96     30.6    29.0   31.7
+//          4     3001 to 8191     32     31.4    26.9   29.2
+//          8     3001 to 8191     20     31.1    31.1   31.6
+//          8     3001 to 8191     64     45.5    50.4   46.1
+//          8     3001 to 8191     96     66.8    73.0   62.9
+//         16     3001 to 8191     40     93.4    98.2   88.8
+//  - `least`: as many parts as are resident with two row tiles (the 96 rows of
+//    8 sequences take 69.7 with two a CU), two a CU with one.
 // More sequences, or few positions: by the longest one's length, about a
 // thousand workgroups.  Up to 512 positions (384 with two row tiles) stay in
-// one part, which needs no second launch (one sequence, 8 heads of 128, 4
-// query heads each, us in a graph: 200 positions 7.5 and 9.0, 384 8.6 and 9.3,
-// 512 9.6 and 9.1, 768 11.4 and 9.6; a launch from Python is 3 more).
-// Four row tiles a wave spill.
+// one part, which needs no second launch, and that is 3 more from Python (one
+// sequence, 4 query heads a head: 200 positions 7.7 and 8.9 in two launches, 384
+// 8.9 and 9.2, 512 10.1 and 9.0, 768 12.2 and 9.6; 48 rows: 200 positions 11.3
+// and 12.0, 384 13.2 and 12.3, 512 15.0 and 12.1).
+// Four row tiles a wave spill, and so do two with 8-bit heads of 256 elements
+// (32 bytes a lane).
 KvSplit kv_split(const KvDims& d, int32_t q_heads, int64_t B, int64_t max_q, int64_t max_kv) {
   const int64_t rows = max_q * (q_heads / d.heads);
   KvSplit s;
@@ -977,8 +987,9 @@ void launch_attend(const KvAttend& a, const KvSplit& s, hipStream_t stream) {
   else k_kv_attend<D, BITS, 2><<<grid, block, pad, stream>>>(a, s);
   if (s.parts <= 1) return;
   const int64_t x = (int64_t)a.T * a.q_heads;
-  // a wave a row, or four where rows are few and parts many (16 sequences of
-  // 501 to 2191 positions, 4096 rows: 24.7 us a call and 29.1)
+  // a wave a row, or four where rows are few and parts many (us a call, a wave
+  // and four: 16 sequences of 501 to 2191 positions, 4096 rows, 26.8 and 31.2;
+  // one token over 200000 positions 122 and 98)
   if (s.parts <= 8 || (s.parts <= 32 && x >= 2048)) k_kv_join<D, 1><<<(unsigned)((x + 3) / 4), 256, 0, stream>>>(a, s);
   else k_kv_join<D, 4><<<(unsigned)x, 256, 0, stream>>>(a, s);
 }
