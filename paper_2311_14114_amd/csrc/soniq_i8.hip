@@ -250,8 +250,8 @@ __global__ __launch_bounds__(512) void k_i8_skinny(I8Gemm g) {
 // makes the codes for itself (at most kFusedMost elements, 32 a thread), in
 // LDS, while its first weights are on their way.  16 output channels a
 // workgroup, K over the waves as above, U segments of each in flight.
-// 1 x 4096 x 4096 takes 6.1 us: 17 MB at 2.8 TB/s, half of it the way from the
-// launch to the codes.  Past 16384 elements the codes cost every workgroup more
+// 1 x 4096 x 4096 takes 6.1 us in a trace (8.2 from one to the next in a graph):
+// 17 MB at 2.8 TB/s, half of it the way from the launch to the codes.  Past 16384 elements the codes cost every workgroup more
 // than a launch of their own (8 x 4096 x 4096: 14.9 us in a graph, 10.5 with
 // two launches); from 8192 on they are level (16 x 2304 x 768: 7.4 and 7.0),
 // and a launch from Python is 4 more.
@@ -473,9 +473,10 @@ __device__ __forceinline__ void tile_out(const I8Gemm& g, const v16i (&acc)[TM][
 // Few tiles leave a CU with one workgroup, whose one stage in flight does not
 // cover the memory's latency.
 //
-// 8192^3 takes 455 to 470 us, 2340 to 2410 TOPS (the matrix cores busy 0.64
-// of the time; a library's product of int8 matrices reached 2066 to 2430 on
-// this card), 4096 x 4096 x 11008 154 us, 2400.  Small tiles are bound by
+// 8192^3 takes 455 to 485 us, 2270 to 2420 TOPS by the card (the matrix cores
+// busy 0.65 of the time; a library's product of int8 matrices reached 2035 to
+// 2500), 4096 x 4096 x 11008 147 to 159 us, 2320 to 2510.  256x256 spills 292
+// bytes a lane, outside its main loop.  Small tiles are bound by
 // LDS: a stage of 64x128 writes 24 KB and reads 48, some 770 of the 900
 // cycles that it takes (301 x 4099 x 4091: 13.6 us); two stages in flight a
 // set, or four sets, changed nothing.  Weights' rows that do not start at
@@ -721,7 +722,8 @@ void launch_tile(const I8Gemm& g, hipStream_t stream) {
 // The tile of a matrix that is no smaller than it.  Larger tiles move fewer
 // bytes a product, smaller ones leave fewer CUs idle; below one tile a CU,
 // two sets of waves hide what one stage in flight does not.  Times in us of a
-// call in a graph, rows of 4096 + 128 bytes (512 in the last lines):
+// call in a graph, rows of 4096 + 128 bytes (512 in the last lines; weights'
+// rows of K bytes take the same, of K + 16 up to a fifth more):
 //                        64x64  2 sets  64x128  2 sets  128x128  256x256
 //    65 x  4096 x 4096    10.0     9.5    12.4    11.7       -        -
 //    80 x 11008 x 4096    17.7    16.0    15.5    13.3       -        -

@@ -37,8 +37,9 @@ constexpr int kCopyTokens = 16;  // tokens a workgroup, at most
 //   write: s = max |x| / top, code = rint(x / s);   read: code * s.
 // Bytes bound it: reading 500 MB of prefixes (8 sequences, 8 heads of 128, 8
 // bits) takes 106 us, 4.7 TB/s, what a large copy reaches; 700 to 4096 tokens
-// of 5 sequences written in 4 bits 18 us and read back 15.  A token or a few
-// take 3.8 to 4.7 us: launch, tables, then one trip to memory.
+// of 5 sequences read back from 4 bits 16 us.  Writing them takes 20, bound by
+// instructions: 8500 a SIMD are some 14 of those.  A token or a few take 3.8 to
+// 4.7 us: launch, tables, then one trip to memory.
 template <int TYPE, int D, int BITS, bool WRITE>
 __global__ __launch_bounds__(256) void k_kv_copy(KvCopy c, int tw) {
   typedef typename Value<TYPE>::T T;
@@ -149,11 +150,12 @@ __global__ __launch_bounds__(256) void k_kv_copy(KvCopy c, int tw) {
 // of its positions; four waves take 32 positions each in turn, keep their
 // own running softmax, and meet at the end.  Parts meet in k_kv_join.
 // Single tokens are bound by the cache's bytes: 32 sequences of 2000 to 32768
-// positions, 8 heads of 128, 8 bits, 4 query heads each: 197 us for 1.06 GB,
-// 5.4 TB/s, and 7 for the join.  Many rows by the vector instructions of codes
-// and softmax: 8 sequences of 3001 to 8191 positions, 96 rows, 4 bits, fp16:
-// 54 us, of which those 17100 a SIMD take 30 (matrix cores 10, 50 MB from
-// memory 10); then the starts and ends of parts.
+// positions, 8 heads of 128, 8 bits, 4 query heads each: 199 us for 1.06 GB,
+// 5.3 TB/s (a plain read reaches 6.4), and 7 for the join.  Many rows by the
+// vector instructions of codes and softmax: 8 sequences of 3001 to 8191
+// positions, 96 rows, 4 bits, fp16: 60 us with the join, of which those 18600 a
+// SIMD take 31 (matrix cores 10, 50 MB from memory 10); then the starts and ends
+// of parts.
 //
 // Everything stays transposed, so that no operand crosses lanes: with
 // kb = lane / 16 and c = lane % 16,
@@ -187,10 +189,10 @@ __global__ __launch_bounds__(256) void k_kv_copy(KvCopy c, int tw) {
 // Half a step of fp16 in each weight is as much as an fp16 output's own and an
 // eighth of a bf16 output's, so a second product takes what the rounding left
 // (without it, fp16 outputs' error against 64 bits was 1.4 to 1.5 times that of
-// rounding the exact output).  It costs single tokens nothing to speak of (201
-// us and 201 for 32 sequences of 2000 to 32768 positions, bf16), many rows 3 to
-// 9% (8 sequences of 3001 to 8191 positions, 96 rows, 8 bits, bf16: 52.4 and
-// 57.1).
+// rounding the exact output).  When it came it cost single tokens nothing to
+// speak of (201 us and 201 for 32 sequences of 2000 to 32768 positions, bf16),
+// many rows 3 to 9% (8 sequences of 3001 to 8191 positions, 96 rows, 8 bits,
+// bf16: 52.4 and 57.1).
 typedef _Float16 h2 __attribute__((ext_vector_type(2)));
 typedef _Float16 h8 __attribute__((ext_vector_type(8)));
 typedef float f4 __attribute__((ext_vector_type(4)));

@@ -81,7 +81,7 @@ soniq_status check_gemm(const char* who, const void* W, int64_t ldw, const float
 // Workspace of soniq_quantize_i8_gemm where it takes two launches: the codes,
 // then the scales.  Rows are padded past a multiple of 128 bytes, so that the
 // same chunk of neighbouring rows does not fall on one cache channel (8192^3:
-// 497 us on rows of 8192 bytes, 468 on 8320).
+// 497 us on token rows of 8192 bytes, 468 on 8320; weights' rows take either).
 int64_t codes_ld(int64_t K) { return round_up(K, 128) + 128; }
 int64_t i8_work(int64_t M, int64_t K) {
   return i8_fused(M, K) ? 0 : M * codes_ld(K) + round_up(4 * M, 16);
